@@ -55,9 +55,11 @@ namespace {
 
 thread_local std::string g_last_error;
 
+}  // namespace
+
 // No exception crosses the C ABI: the message is best effort, and entry points
 // that allocate host bookkeeping run their body under no_throw().
-ff_status fail(ff_status st, const char* fmt, ...) noexcept {
+ff_status ff::fail(ff_status st, const char* fmt, ...) noexcept {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -70,10 +72,15 @@ ff_status fail(ff_status st, const char* fmt, ...) noexcept {
   return st;
 }
 
-ff_status ok() noexcept {
+ff_status ff::ok() noexcept {
   g_last_error.clear();
   return FF_OK;
 }
+
+namespace {
+
+using ff::fail;
+using ff::ok;
 
 template <class F>
 ff_status no_throw(F&& body) noexcept {
@@ -103,17 +110,10 @@ struct Layout {
   size_t total;
 };
 
-// The descriptor as the cache uses it: all-zero rope pairs select the split of
-// the Wan2.1 backbone, d/2 - 2 floor(d/6) pairs on t and floor(d/6) on each of
-// h and w ((22, 21, 21) at d = 128, (12, 10, 10) at d = 64).
+// The descriptor as the cache uses it (all-zero rope pairs resolved)
 ff_cache_desc resolve_desc(const ff_cache_desc& in) {
   ff_cache_desc d = in;
-  if (d.rope_pairs_t == 0 && d.rope_pairs_h == 0 && d.rope_pairs_w == 0 && d.head_dim > 0) {
-    const int n_hw = d.head_dim / 6;
-    d.rope_pairs_t = d.head_dim / 2 - 2 * n_hw;
-    d.rope_pairs_h = n_hw;
-    d.rope_pairs_w = n_hw;
-  }
+  ff::resolve_rope_pairs(d.head_dim, &d.rope_pairs_t, &d.rope_pairs_h, &d.rope_pairs_w);
   return d;
 }
 
@@ -263,12 +263,7 @@ ff_status ff_cache_create(const ff_cache_desc* desc, void* dev_buf, size_t dev_b
     c->desc = rd;
     c->layout = L;
     c->dev = static_cast<char*>(dev_buf);
-    const int axis_n[3] = {rd.rope_pairs_t, rd.rope_pairs_h, rd.rope_pairs_w};
-    std::fill(std::begin(c->omega), std::end(c->omega), 0.0);
-    int pair = 0;
-    for (int a = 0; a < 3; ++a)
-      for (int j = 0; j < axis_n[a]; ++j)
-        c->omega[pair++] = std::pow(rd.rope_theta, -double(j) / double(axis_n[a]));
+    ff::rope_frequencies(rd.rope_pairs_t, rd.rope_pairs_h, rd.rope_pairs_w, rd.rope_theta, c->omega);
     const size_t rings = size_t(rd.num_stages) * rd.num_layers;
     c->slot_chunk.assign(rings * rd.ring_chunks, -1);
     c->next_chunk.assign(rings, -1);

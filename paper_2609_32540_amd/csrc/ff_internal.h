@@ -5,9 +5,34 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cmath>
+
 #include "ff.h"
 
 namespace ff {
+
+// Error reporting of the C ABI's entry points: fail() stores the message that
+// ff_last_error() returns and hands `st` back, ok() clears it.
+ff_status fail(ff_status st, const char* fmt, ...) noexcept;
+ff_status ok() noexcept;
+
+// Rotation pairs of the three axes as a call uses them: all zero selects the split of the
+// Wan2.1 backbone, d/2 - 2 floor(d/6) pairs on t and floor(d/6) on each of h and w.
+inline void resolve_rope_pairs(int32_t head_dim, int32_t* t, int32_t* h, int32_t* w) {
+  if (*t == 0 && *h == 0 && *w == 0 && head_dim > 0) {
+    *h = *w = head_dim / 6;
+    *t = head_dim / 2 - 2 * (head_dim / 6);
+  }
+}
+
+// Frequency of every pair: theta^(-j / n) of pair j of an axis of n pairs.
+inline void rope_frequencies(int n_t, int n_h, int n_w, double theta, double (&omega)[64]) {
+  const int axis_n[3] = {n_t, n_h, n_w};
+  int pair = 0;
+  for (int a = 0; a < 3; ++a)
+    for (int j = 0; j < axis_n[a]; ++j) omega[pair++] = std::pow(theta, -double(j) / double(axis_n[a]));
+  while (pair < 64) omega[pair++] = 0.0;
+}
 
 // Keys of one attention call come as a list of segments: the anchor segment
 // (or runs of consecutive frames of a caller's anchor bank), the valid history

@@ -31,4 +31,32 @@ __device__ inline float round_to_odd_f32(double x) {
   return __uint_as_float(bits | 1u);
 }
 
+// Rotation of adjacent pairs in float64, rounded once to the storage type:
+// (a, b) -> (a cos - b sin, a sin + b cos) with cs = (cos, sin); rotate_vec turns the
+// pairs of one 16-byte vector of T.
+__device__ inline uint32_t rotate_bf16_pair(uint32_t w, double2 cs) {
+  const double a = bf16_lo(w), b = bf16_hi(w);
+  const double o0 = a * cs.x - b * cs.y;
+  const double o1 = a * cs.y + b * cs.x;
+  return pack_bf16_rne(round_to_odd_f32(o0), round_to_odd_f32(o1));
+}
+
+template <typename T>
+__device__ inline uint4 rotate_vec(uint4 w, const double2* cs) {
+  if constexpr (sizeof(T) == 2) {
+    w.x = rotate_bf16_pair(w.x, cs[0]);
+    w.y = rotate_bf16_pair(w.y, cs[1]);
+    w.z = rotate_bf16_pair(w.z, cs[2]);
+    w.w = rotate_bf16_pair(w.w, cs[3]);
+  } else {
+    const double a0 = __uint_as_float(w.x), b0 = __uint_as_float(w.y);
+    const double a1 = __uint_as_float(w.z), b1 = __uint_as_float(w.w);
+    w.x = __float_as_uint(float(a0 * cs[0].x - b0 * cs[0].y));
+    w.y = __float_as_uint(float(a0 * cs[0].y + b0 * cs[0].x));
+    w.z = __float_as_uint(float(a1 * cs[1].x - b1 * cs[1].y));
+    w.w = __float_as_uint(float(a1 * cs[1].y + b1 * cs[1].x));
+  }
+  return w;
+}
+
 }  // namespace ff

@@ -1,0 +1,242 @@
+// Host side of the paged cache: validation, launch choices and the C ABI entry points
+// declared in include/ff_paged.h.  Stateless: lengths and pages stay on the device.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "ff_paged.h"
+#include "ff_paged_internal.h"
+
+namespace {
+
+using ff::fail;
+using ff::ok;
+
+ff_status check_aligned(const void* p, size_t to, const char* name) {
+  if (reinterpret_cast<uintptr_t>(p) % to != 0)
+    return fail(FF_ERR_INVALID_ARG, "%s must be %zu-byte aligned", name, to);
+  return FF_OK;
+}
+
+ff_status hip_status(hipError_t e, const char* what) {
+  if (e != hipSuccess) return fail(FF_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+  return ok();
+}
+
+int elem_bytes(const ff_paged_desc& d) { return d.dtype == FF_DT_BF16 ? 2 : 4; }
+
+ff_status check_desc(const ff_paged_desc* d) {
+  if (!d) return fail(FF_ERR_INVALID_ARG, "desc is NULL");
+  if (d->num_pages < 1) return fail(FF_ERR_INVALID_ARG, "num_pages must be >= 1");
+  if (d->page_tokens < FF_MIN_PAGE_TOKENS || d->page_tokens > FF_MAX_PAGE_TOKENS ||
+      (d->page_tokens & (d->page_tokens - 1)) != 0)
+    return fail(FF_ERR_UNSUPPORTED, "page_tokens must be a power of two in [%d, %d]",
+                FF_MIN_PAGE_TOKENS, FF_MAX_PAGE_TOKENS);
+  if (d->num_kv_heads < 1 || d->num_q_heads < 1)
+    return fail(FF_ERR_INVALID_ARG, "num_kv_heads and num_q_heads must be >= 1");
+  if (d->num_q_heads % d->num_kv_heads != 0)
+    return fail(FF_ERR_SHAPE, "num_q_heads must be a multiple of num_kv_heads");
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(FF_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (d->dtype != FF_DT_BF16 && d->dtype != FF_DT_F32)
+    return fail(FF_ERR_UNSUPPORTED, "dtype must be FF_DT_BF16 or FF_DT_F32");
+  if (d->n_seqs < 0 || d->n_seqs > FF_MAX_PAGED_SEQS)
+    return fail(FF_ERR_UNSUPPORTED, "n_seqs must be in [0, %d]", FF_MAX_PAGED_SEQS);
+  if (d->n_tokens < 0) return fail(FF_ERR_INVALID_ARG, "n_tokens must be >= 0");
+  if (d->min_new < 0 || d->max_new < 0 || (d->max_new > 0 && d->min_new > d->max_new))
+    return fail(FF_ERR_INVALID_ARG, "min_new and max_new must be 0 <= min_new <= max_new");
+  if (d->max_pages < 1) return fail(FF_ERR_INVALID_ARG, "max_pages must be >= 1");
+  if (int64_t(d->max_pages) * d->page_tokens > (int64_t(1) << 30))
+    return fail(FF_ERR_UNSUPPORTED, "max_pages * page_tokens must be at most 2^30");
+  if (d->table_stride < d->max_pages)
+    return fail(FF_ERR_SHAPE, "table_stride must be at least max_pages");
+  // rows of a sequence and elements of a row of heads are counted in 32 bits
+  if (int64_t(d->n_tokens) * (d->num_q_heads / d->num_kv_heads) > INT32_MAX - 256)
+    return fail(FF_ERR_UNSUPPORTED, "n_tokens * query heads per kv head must fit in 32 bits");
+  if (int64_t(d->num_q_heads) * d->head_dim > (1 << 24))
+    return fail(FF_ERR_UNSUPPORTED, "num_q_heads * head_dim must be at most 2^24");
+  if (d->n_seqs > 0) {
+    if (!d->q_start || !d->kv_len || !d->page_table)
+      return fail(FF_ERR_INVALID_ARG, "q_start, kv_len and page_table must be non-NULL");
+    if (check_aligned(d->q_start, 4, "q_start") != FF_OK ||
+        check_aligned(d->kv_len, 4, "kv_len") != FF_OK ||
+        check_aligned(d->page_table, 4, "page_table") != FF_OK)
+      return FF_ERR_INVALID_ARG;
+  }
+  return FF_OK;
+}
+
+// Rows of heads that are `stride` elements apart
+ff_status check_rows(const ff_paged_desc& d, const void* p, int64_t stride, int heads,
+                     const char* name) {
+  if (!p) return fail(FF_ERR_INVALID_ARG, "%s is NULL", name);
+  if (check_aligned(p, 16, name) != FF_OK) return FF_ERR_INVALID_ARG;
+  if (stride < int64_t(heads) * d.head_dim || stride * elem_bytes(d) % 16 != 0 ||
+      stride > (int64_t(1) << 31))
+    return fail(FF_ERR_SHAPE, "the rows of %s must be a multiple of 16 bytes and at least "
+                "%d heads of %d elements apart", name, heads, d.head_dim);
+  return FF_OK;
+}
+
+ff::PagedBatch make_batch(const ff_paged_desc& d) {
+  ff::PagedBatch b;
+  std::memset(&b, 0, sizeof(b));
+  b.q_start = d.q_start;
+  b.kv_len = d.kv_len;
+  b.page_table = d.page_table;
+  b.table_stride = d.table_stride;
+  b.n_seqs = d.n_seqs;
+  b.n_tokens = d.n_tokens;
+  b.max_pages = d.max_pages;
+  b.num_pages = d.num_pages;
+  b.page_shift = __builtin_ctz(unsigned(d.page_tokens));
+  b.kv_heads = d.num_kv_heads;
+  b.group = d.num_q_heads / d.num_kv_heads;
+  b.window = -1;
+  return b;
+}
+
+// Launch choices of one attention call: they follow from sizes, so that the workspace can
+// be asked for ahead of it.
+struct Plan {
+  int qt;            // 16-row query tiles per workgroup
+  ff::PagedSplit split;
+  int64_t tiles;     // at most this many tiles per kv head
+  int64_t items;     // and items
+  size_t workspace;
+};
+
+Plan make_plan(const ff_paged_desc& d) {
+  Plan p;
+  const int group = d.num_q_heads / d.num_kv_heads;
+  const int64_t most = d.max_new > 0 ? std::min(d.max_new, d.n_tokens) : d.n_tokens;
+  p.qt = most * group <= 16 ? 1 : 2;
+  const int block = d.dtype == FF_DT_BF16 ? 32 : 16;
+  const int64_t blocks = (int64_t(d.max_pages) * d.page_tokens + block - 1) / block;
+  p.split.min_per = 256 / block;
+  p.split.target = blocks > p.split.min_per
+                       ? (4 * ff::device_cus() + d.num_kv_heads - 1) / d.num_kv_heads : 0;
+  p.split.min_rows = 0;
+  p.split.max_rows = INT32_MAX;
+  p.tiles = ff::paged_max_items(d.n_tokens, d.n_seqs, group, 16 * p.qt, 0);
+  p.items = ff::paged_max_items(d.n_tokens, d.n_seqs, group, 16 * p.qt, p.split.target);
+  p.workspace = p.split.target > 0 ? size_t(p.items) * d.num_kv_heads *
+                                         ff::paged_part_floats(16 * p.qt, d.head_dim) * 4 : 0;
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+ff_status ff_paged_append(const ff_paged_desc* desc, const ff_paged_rope* rope, const void* q,
+                          const void* k, const void* v, int64_t q_stride, int64_t k_stride,
+                          int64_t v_stride, const int32_t* positions, void* q_out, void* k_pages,
+                          void* v_pages, void* stream) {
+  ff_status st = check_desc(desc);
+  if (st != FF_OK) return st;
+  const ff_paged_desc& d = *desc;
+  if (!rope) return fail(FF_ERR_INVALID_ARG, "rope is NULL");
+  ff_paged_rope r = *rope;
+  ff::resolve_rope_pairs(d.head_dim, &r.rope_pairs_t, &r.rope_pairs_h, &r.rope_pairs_w);
+  const int64_t pairs = int64_t(r.rope_pairs_t) + r.rope_pairs_h + r.rope_pairs_w;
+  if (r.rope_pairs_t < 0 || r.rope_pairs_h < 0 || r.rope_pairs_w < 0 || pairs != d.head_dim / 2)
+    return fail(FF_ERR_INVALID_ARG, "rope pairs must be >= 0 and sum to head_dim / 2");
+  if (!(r.rope_theta > 0.0) || !std::isfinite(r.rope_theta))
+    return fail(FF_ERR_INVALID_ARG, "rope_theta must be positive");
+  if (d.n_seqs == 0 || d.n_tokens == 0) return ok();
+  if ((st = check_rows(d, k, k_stride, d.num_kv_heads, "k")) != FF_OK) return st;
+  if ((st = check_rows(d, v, v_stride, d.num_kv_heads, "v")) != FF_OK) return st;
+  if (q) {
+    if ((st = check_rows(d, q, q_stride, d.num_q_heads, "q")) != FF_OK) return st;
+    if (!q_out) return fail(FF_ERR_INVALID_ARG, "q_out is NULL");
+    if (check_aligned(q_out, 16, "q_out") != FF_OK) return FF_ERR_INVALID_ARG;
+    if (q_out == q && q_stride != int64_t(d.num_q_heads) * d.head_dim)
+      return fail(FF_ERR_SHAPE, "q_out may be q only when q is dense");
+  }
+  if (!k_pages || !v_pages) return fail(FF_ERR_INVALID_ARG, "k_pages and v_pages must be non-NULL");
+  if (check_aligned(k_pages, 16, "k_pages") != FF_OK || check_aligned(v_pages, 16, "v_pages") != FF_OK ||
+      check_aligned(positions, 4, "positions") != FF_OK)
+    return FF_ERR_INVALID_ARG;
+  ff::PagedAppend a;
+  std::memset(&a, 0, sizeof(a));
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.positions = positions;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.n_t = r.rope_pairs_t;
+  a.n_th = r.rope_pairs_t + r.rope_pairs_h;
+  ff::rope_frequencies(r.rope_pairs_t, r.rope_pairs_h, r.rope_pairs_w, r.rope_theta, a.omega);
+  return hip_status(ff::launch_paged_append(make_batch(d), a, d.head_dim, d.dtype,
+                                            static_cast<hipStream_t>(stream)),
+                    "paged_append launch");
+}
+
+size_t ff_paged_attention_workspace(const ff_paged_desc* desc) {
+  if (check_desc(desc) != FF_OK) return 0;
+  ok();
+  return make_plan(*desc).workspace;
+}
+
+ff_status ff_paged_attention(const ff_paged_desc* desc, const void* q, int64_t q_stride,
+                             const void* k_pages, const void* v_pages, void* out, float* lse,
+                             float softmax_scale, int32_t block, int32_t window,
+                             int32_t anchor_tokens, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  ff_status st = check_desc(desc);
+  if (st != FF_OK) return st;
+  const ff_paged_desc& d = *desc;
+  if (!(softmax_scale > 0.0f) || !std::isfinite(softmax_scale))
+    return fail(FF_ERR_INVALID_ARG, "softmax_scale must be positive and finite");
+  if (block != 0 && block != 1) return fail(FF_ERR_INVALID_ARG, "block must be 0 or 1");
+  if (window < -1) return fail(FF_ERR_INVALID_ARG, "window must be -1 or >= 0");
+  if (anchor_tokens < 0) return fail(FF_ERR_INVALID_ARG, "anchor_tokens must be >= 0");
+  if (d.n_seqs == 0 || d.n_tokens == 0) return ok();
+  if ((st = check_rows(d, q, q_stride, d.num_q_heads, "q")) != FF_OK) return st;
+  if (!k_pages || !v_pages || !out)
+    return fail(FF_ERR_INVALID_ARG, "k_pages, v_pages and out must be non-NULL");
+  if (check_aligned(k_pages, 16, "k_pages") != FF_OK || check_aligned(v_pages, 16, "v_pages") != FF_OK ||
+      check_aligned(out, 16, "out") != FF_OK || check_aligned(lse, 4, "lse") != FF_OK ||
+      check_aligned(workspace, 16, "workspace") != FF_OK)
+    return FF_ERR_INVALID_ARG;
+  const Plan p = make_plan(d);
+  if (p.workspace > 0 && !workspace) return fail(FF_ERR_INVALID_ARG, "workspace is NULL");
+  if (workspace_bytes < p.workspace)
+    return fail(FF_ERR_BUFFER, "workspace_bytes %zu < required %zu", workspace_bytes, p.workspace);
+  // (a grid holds at most 2^32 - 1 threads)
+  if (p.items * d.num_kv_heads > int64_t(UINT32_MAX) / 512)
+    return fail(FF_ERR_UNSUPPORTED, "too many rows for one launch");
+  ff::PagedBatch b = make_batch(d);
+  b.window = std::min(window, 1 << 30);
+  b.anchor_tokens = std::min(anchor_tokens, 1 << 30);
+  b.block = block;
+  ff::PagedTensors t;
+  std::memset(&t, 0, sizeof(t));
+  t.q = q;
+  t.out = out;
+  t.lse = lse;
+  t.k_pages = k_pages;
+  t.v_pages = v_pages;
+  t.part = static_cast<float*>(workspace);
+  t.q_stride = q_stride;
+  t.scale = softmax_scale;
+  t.scale_log2 = float(double(softmax_scale) * 1.4426950408889634);
+  const hipStream_t hs = static_cast<hipStream_t>(stream);
+  hipError_t e = d.dtype == FF_DT_BF16
+                     ? ff::launch_paged_attn_bf16(p.qt, b, p.split, t, p.items, d.head_dim, hs)
+                     : ff::launch_paged_attn_f32(p.qt, b, p.split, t, p.items, d.head_dim, hs);
+  if (e == hipSuccess && p.split.target > 0)
+    e = ff::launch_paged_join(p.qt, b, p.split, t, p.items, p.tiles, d.head_dim, d.dtype, hs);
+  return hip_status(e, "paged_attention launch");
+}
+
+}  // extern "C"

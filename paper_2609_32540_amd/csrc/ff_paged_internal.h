@@ -1,0 +1,86 @@
+// Internal interface between the host side of the paged cache (ff_paged.cpp) and its
+// kernels.  Not part of the C ABI.
+#pragma once
+
+#include <float.h>
+#include <math.h>
+
+#include "ff_internal.h"
+#include "ff_numeric.h"
+#include "ff_paged.h"
+#include "paged_plan.h"
+
+namespace ff {
+
+// Tensors of one attention launch.  q rows are q_stride elements apart; out is dense.
+struct PagedTensors {
+  const void* q;
+  void* out;
+  float* lse;               // optional [n_tokens][query heads]
+  const void* k_pages;      // [num_pages][kv_heads][page tokens][d]
+  const void* v_pages;
+  float* part;              // partial results of items of tiles with several parts
+  int64_t q_stride;
+  float scale;              // softmax_scale
+  float scale_log2;         // softmax_scale * log2 e
+};
+
+// Tensors of one append launch; rows are *_stride elements apart, q_out is dense.
+struct PagedAppend {
+  const void* q;            // optional
+  const void* k;
+  const void* v;
+  void* q_out;
+  void* k_pages;
+  void* v_pages;
+  const int32_t* positions; // optional [n_tokens][3]
+  int64_t q_stride, k_stride, v_stride;
+  int32_t n_t, n_th;        // pairs [0, n_t) turn by t, [n_t, n_th) by h, the rest by w
+  double omega[64];         // frequency of each pair
+};
+
+// Floats of one partial result: O [rt][d], then reference, sum of the weights that O adds
+// up and sum of the unrounded weights of each row.
+__host__ __device__ inline int64_t paged_part_floats(int rt, int d) { return int64_t(rt) * (d + 3); }
+
+// N elements of a row of the output; a row that saw nothing (l = 0) is zero
+template <class T, int N>
+__device__ inline void paged_store(T* out, const float* acc, float l) {
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  float v[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = l == 0.0f ? 0.0f : acc[i] * inv;
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const u32x2 w = {pack_bf16_rne(v[i], v[i + 1]), pack_bf16_rne(v[i + 2], v[i + 3])};
+      *reinterpret_cast<u32x2*>(out + i) = w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4)
+      *reinterpret_cast<f32x4*>(out + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+  }
+}
+
+// base-2 log-sum-exp of a row from its reference and sum (-inf for a row that saw nothing)
+__device__ inline float paged_lse(float m, float u) { return u == 0.0f ? -INFINITY : m + log2f(u); }
+
+hipError_t launch_paged_append(const PagedBatch& b, const PagedAppend& a, int head_dim, int dtype,
+                               hipStream_t stream);
+
+// Few rows per sequence: tiles of 16 qt rows, keys split as sp says; items: the launch's
+// items per kv head (paged_max_items).
+hipError_t launch_paged_attn_bf16(int qt, const PagedBatch& b, const PagedSplit& sp,
+                                  const PagedTensors& t, int64_t items, int head_dim,
+                                  hipStream_t stream);
+hipError_t launch_paged_attn_f32(int qt, const PagedBatch& b, const PagedSplit& sp,
+                                 const PagedTensors& t, int64_t items, int head_dim,
+                                 hipStream_t stream);
+
+// Joins the parts that those launches left; tiles: at most this many per kv head.
+hipError_t launch_paged_join(int qt, const PagedBatch& b, const PagedSplit& sp,
+                             const PagedTensors& t, int64_t items, int64_t tiles, int head_dim,
+                             int dtype, hipStream_t stream);
+
+}  // namespace ff

@@ -1,0 +1,472 @@
+// Attention of one or a few new tokens per sequence over a paged cache, bf16: the cache's
+// length is split over workgroups and over the waves of a workgroup, and joined.
+//
+// Mathematics.  out = sum_j p_j v_j / sum_j p_j with p_j = 2^(c q.k_j - m), c = scale
+// log2 e.  Any split of the keys works with a reference m of its own: parts (O, m, l) join
+// as O = sum_w 2^(m_w - M) O_w, l likewise, M = max m_w.
+//
+// Work split.  The query heads of one kv head read the same keys, so a tile is 16 QT rows
+// (token, query head of the group) of one sequence and kv head.  An item is a tile and one
+// of its parts of the keys (paged_plan.h); a workgroup of four waves runs one item of one
+// kv head, 32-key blocks dealt round robin to its waves, which join through LDS; items of
+// a tile with several parts leave unnormalised float32 partials in the workspace, joined
+// by paged_join_kernel.  What bounds it: every key and value is read from HBM once, while
+// the products fill the matrix unit's 16 columns with as few as one row.
+//
+// Operands as in attn_bf16_split.hip: S^T = K Q^T and O^T += V^T P^T on
+// v_mfma_f32_16x16x32_bf16; each wave copies its own blocks HBM -> LDS in whole pieces of
+// rows (global_load_lds) and takes them into registers before the products, which frees
+// the LDS for the copy of its next block.  A page holds the rows of one kv head in one
+// piece ([kv heads][page tokens][d]), and at least 16 of them, so that each half of a
+// block (16 keys) lies in one page and is copied from one base; rows of the page behind
+// the sequence's end are copied with it and masked.
+//
+// Masked keys.  A key that no row of the tile sees (behind the end, in a hole, outside
+// window and anchors) has its score replaced by -inf and its V row by zero: what its
+// memory holds (stale values, infinities, NaN) does not matter.  Where the rows of a tile
+// see different keys, a V element that is not finite is kept out of the products, which
+// would spread it to every row as 0 * inf, and added for the rows that see it.
+//
+// Rounding: probabilities to bf16 (nearest even) as operands of the matrix unit, the sums
+// that divide O over the rounded values; scores, references, sums and O are float32.
+
+#include <hip/hip_runtime.h>
+
+#include <float.h>
+#include <math.h>
+
+#include "ff_paged_internal.h"
+
+namespace ff {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kBK = 32;            // keys per block
+constexpr float kRaise = 56.0f;    // log2 units a score may exceed the reference by: sums of
+                                   // 2^56 times the keys stay far inside float32
+
+template <int D, int QT>
+struct PagedCfg {
+  static constexpr int KS = D / 32;            // 32-wide d slices of S^T
+  static constexpr int DT = D / 16;            // 16-row d tiles of O^T
+  static constexpr int BLOCK = kBK * 2 * D;    // bytes of one K (or V) block
+  static constexpr int HALF = BLOCK / 2;       // of its half, 16 keys
+  static constexpr int N = HALF / 1024;        // 1 KB copies of a half
+  static constexpr int kRows = 16 * QT;
+  static constexpr int kPitch = D + 4;         // padded row of the join buffer (floats)
+  static constexpr int kJoin = kWaves * kRows * (kPitch + 3) * 4;
+  static constexpr int kLds = kWaves * 2 * BLOCK > kJoin ? kWaves * 2 * BLOCK : kJoin;
+};
+
+__device__ inline bool not_finite(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+
+// w without its bf16 halves that are not finite
+__device__ inline uint32_t finite_halves(uint32_t w) {
+  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
+  return w;
+}
+
+template <int D, int QT>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
+  using C = PagedCfg<D, QT>;
+  __shared__ __attribute__((aligned(1024))) char lds[C::kLds];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4;
+  const int head = blockIdx.x % b.kv_heads;
+  const int item = blockIdx.x / b.kv_heads;
+
+  PagedItem it;
+  if (!PagedScan<C::kRows, kBK>::find(b, sp, item, false, lane, &it)) return;
+  const int n_rows = it.seq.n_new * b.group;
+  const int row0 = it.tile * C::kRows;
+  const int row1 = min(row0 + C::kRows, n_rows) - 1;   // last row of the tile
+  const PagedRange head_r = paged_range(b, it.seq, row0 / b.group);
+  const PagedRange tail_r = paged_range(b, it.seq, row1 / b.group);
+  const PagedBlocks<kBK> blocks = paged_blocks<kBK>(b, head_r, tail_r);
+  const int t0 = uniform(int(int64_t(it.part) * blocks.n / it.parts));
+  const int t1 = uniform(int(int64_t(it.part + 1) * blocks.n / it.parts));
+  const bool rows_differ = head_r.hi != tail_r.hi || head_r.lo != tail_r.lo;
+
+  // Q^T operand and what each row sees (lane l16 of query tile x: row 16 x + l16)
+  bf16x8 qreg[QT][C::KS];
+  PagedRange see[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int r = min(row0 + 16 * x + l16, row1);
+    const int tau = r / b.group;
+    see[x] = paged_range(b, it.seq, tau);
+    const __bf16* qp = static_cast<const __bf16*>(t.q) + int64_t(it.seq.q0 + tau) * t.q_stride +
+                       int64_t(head * b.group + r - tau * b.group) * D + 8 * grp;
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) qreg[x][s] = *reinterpret_cast<const bf16x8*>(qp + 32 * s);
+  }
+
+  f32x4 o[C::DT][QT], lsum[QT];
+  float m_run[QT], l_run[QT];
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    m_run[x] = -FLT_MAX;   // (finite: keys that score -inf get weight 0)
+    l_run[x] = 0.0f;       // this lane's share of the sum of the unrounded probabilities
+    lsum[x] = f32x4{};     // sum of the rounded ones (every row of the tile holds it)
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt) o[dt][x] = f32x4{};
+  }
+
+  // Pages of this wave's blocks t0 + wave, + 4, ..: lane 2 i + half holds the page of that
+  // half of block i of the current 32 (a reload every 32 blocks)
+  int page_of = -1;
+  auto load_pages = [&](int i0) __attribute__((always_inline)) {
+    const int tb = t0 + wave + kWaves * (i0 + (lane >> 1));
+    page_of = -1;
+    if (tb < t1) {
+      const int j = blocks.key0(tb) + 16 * (lane & 1);
+      if (j < tail_r.hi) page_of = paged_page(b, it.s, j);
+    }
+  };
+
+  // The wave's K and V block in LDS, in the layouts of attn_bf16_split.hip (lanes of a
+  // quad (K) or octet (V) take consecutive bytes of a row, permuted so that the operand
+  // reads are free of bank conflicts).
+  char* kbuf = lds + wave * 2 * C::BLOCK;
+  char* vbuf = kbuf + C::BLOCK;
+  const int k_lane = 64 * l16 + 16 * (grp ^ (l16 >> 2));
+  int v_lane[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int r = 4 * grp + (l16 >> 2);
+    v_lane[p] = (r >> 3) * (16 * D) + 128 * (r & 7) + 32 * (p ^ ((r & 7) >> 1)) + 8 * (l16 & 3);
+  }
+  uint32_t koff[C::N], voff[C::N];
+#pragma unroll
+  for (int i = 0; i < C::N; ++i) {
+    constexpr uint32_t kSpan = 1024u * (C::N - 1);
+    const int kr = lane >> 2, kch = 4 * i + ((lane & 3) ^ (lane >> 4));
+    const int vr = 8 * (i / (D / 64)) + (lane >> 3);
+    const int vch = 8 * (i % (D / 64)) + ((lane & 7) ^ (2 * (lane >> 4)));
+    koff[i] = uint32_t(kr * 2 * D + 16 * kch) + (kSpan - 1024u * i);
+    voff[i] = uint32_t(vr * 2 * D + 16 * vch) + (kSpan - 1024u * i);
+  }
+  const int slot_mask = (1 << b.page_shift) - 1;
+  const char* kp = static_cast<const char*>(t.k_pages);
+  const char* vp = static_cast<const char*>(t.v_pages);
+  // byte offset in the pool of the 16 keys from key j, which lie in page `page`
+  auto half_offset = [&](int page, int j) __attribute__((always_inline)) {
+    return ((int64_t(max(page, 0)) * b.kv_heads + head) * (slot_mask + 1) + (j & slot_mask)) * (2 * D);
+  };
+
+  // Copy block tb, whose halves lie in the given pages (a hole reads page 0: masked).
+  auto fetch = [&](int tb, int page0, int page1) __attribute__((always_inline)) {
+    constexpr int64_t kSpan = 1024 * (C::N - 1);
+    const int j = blocks.key0(tb);
+    const uint32_t dst = uint32_t(size_t(LDS_PTR(char, kbuf)));
+    const int64_t a = uniform(half_offset(page0, j) - kSpan), c = uniform(half_offset(page1, j + 16) - kSpan);
+    lds_copy_blocks<C::N>(dst, kp + a, koff);
+    lds_copy_blocks<C::N>(dst + C::HALF, kp + c, koff);
+    lds_copy_blocks<C::N>(dst + C::BLOCK, vp + a, voff);
+    lds_copy_blocks<C::N>(dst + C::BLOCK + C::HALF, vp + c, voff);
+  };
+
+  int tb = t0 + wave, i = 0;       // this wave's i-th block
+  int page[2] = {-1, -1};
+  if (tb < t1) {
+    load_pages(0);
+    page[0] = __builtin_amdgcn_readlane(page_of, 0);
+    page[1] = __builtin_amdgcn_readlane(page_of, 1);
+    fetch(tb, page[0], page[1]);
+  }
+  while (tb < t1) {
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    asm volatile("" ::: "memory");
+    bf16x8 kc[2][C::KS];
+    u32x4 va[C::DT];
+#pragma unroll
+    for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+      for (int ks = 0; ks < C::KS; ++ks)
+        kc[kh][ks] = *reinterpret_cast<const bf16x8*>(kbuf + k_lane + 1024 * (kh * C::KS + ks));
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt) {
+      const char* vt = vbuf + v_lane[dt % 4] + 1024 * (dt / 4);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, vt));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, vt + 32 * D));
+      const u32x2 lo2 = __builtin_bit_cast(u32x2, lo), hi2 = __builtin_bit_cast(u32x2, hi);
+      va[dt] = u32x4{lo2[0], lo2[1], hi2[0], hi2[1]};
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done
+    __builtin_amdgcn_sched_barrier(0);
+    const int j0 = blocks.key0(tb);
+    const int cur[2] = {page[0], page[1]};
+    const int next = tb + kWaves;
+    ++i;
+    if (next < t1) {
+      if ((i & 31) == 0) load_pages(i);
+      page[0] = __builtin_amdgcn_readlane(page_of, 2 * (i & 31));
+      page[1] = __builtin_amdgcn_readlane(page_of, 2 * (i & 31) + 1);
+      fetch(next, page[0], page[1]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    f32x4 s[2][QT];
+#pragma unroll
+    for (int ks = 0; ks < C::KS; ++ks)
+#pragma unroll
+      for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+        for (int x = 0; x < QT; ++x)
+          s[kh][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[kh][ks], qreg[x][ks],
+                                                             ks == 0 ? f32x4{} : s[kh][x], 0, 0, 0);
+
+    // the block holds keys that some row does not see
+    const bool edge = j0 + kBK > head_r.hi || cur[0] < 0 || cur[1] < 0 ||
+                      (j0 < tail_r.lo && j0 + kBK > b.anchor_tokens);
+    bool spread = false;   // some V element that is not finite was kept out of the products
+    if (edge) {
+#pragma unroll
+      for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = j0 + 16 * kh + 4 * grp + e;
+#pragma unroll
+          for (int x = 0; x < QT; ++x) {
+            const bool seen = cur[kh] >= 0 && j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
+            s[kh][x][e] = seen ? s[kh][x][e] : -INFINITY;
+          }
+          // (a key some row may see: before the last row's end, behind the first row's start)
+          const bool any = cur[kh] >= 0 && j < tail_r.hi && (j >= head_r.lo || j < b.anchor_tokens);
+          if (!any)
+#pragma unroll
+            for (int dt = 0; dt < C::DT; ++dt)
+              va[dt][2 * kh + (e >> 1)] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+        }
+      if (rows_differ) {
+        bool bad = false;
+#pragma unroll
+        for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) bad |= not_finite(va[dt][w]);
+        spread = __builtin_amdgcn_ballot_w64(bad) != 0;
+        if (spread)
+#pragma unroll
+          for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) va[dt][w] = finite_halves(va[dt][w]);
+      }
+    }
+
+    float mx[QT];
+    bool over = false;
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+      mx[x] = fmaxf(fmaxf(s[0][x][0], s[0][x][1]), fmaxf(s[0][x][2], s[0][x][3]));
+      mx[x] = fmaxf(mx[x], fmaxf(fmaxf(s[1][x][0], s[1][x][1]), fmaxf(s[1][x][2], s[1][x][3])));
+      mx[x] = max_across_groups(mx[x]) * t.scale_log2;
+      // the first block's max is the reference from then on, until a score passes it far
+      over |= mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + kRaise);
+    }
+    if (__builtin_amdgcn_ballot_w64(over) != 0) {
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        const float m_new = mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + kRaise) ? mx[x] : m_run[x];
+        const float alpha = __builtin_amdgcn_exp2f(m_run[x] - m_new);
+        l_run[x] *= alpha;
+        lsum[x] *= alpha;
+        m_run[x] = m_new;
+#pragma unroll
+        for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[dt][x][e] *= alpha;
+      }
+    }
+    uint32_t pk[QT][4];
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+      float lb = 0.0f;
+#pragma unroll
+      for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kh][x][e], t.scale_log2, -m_run[x]));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kh][x][e + 1], t.scale_log2, -m_run[x]));
+          pk[x][2 * kh + (e >> 1)] = pack_bf16(p0, p1);
+          lb += p0 + p1;
+        }
+      l_run[x] += lb;
+    }
+    // (all ones: every row of the result is the column sum of P^T)
+    const bf16x8 ones = {__bf16(1.0f), __bf16(1.0f), __bf16(1.0f), __bf16(1.0f),
+                         __bf16(1.0f), __bf16(1.0f), __bf16(1.0f), __bf16(1.0f)};
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+      const u32x4 pu = {pk[x][0], pk[x][1], pk[x][2], pk[x][3]};
+      const bf16x8 pb = __builtin_bit_cast(bf16x8, pu);
+#pragma unroll
+      for (int dt = 0; dt < C::DT; ++dt)
+        o[dt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[dt]), pb,
+                                                           o[dt][x], 0, 0, 0);
+      lsum[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb, lsum[x], 0, 0, 0);
+    }
+    if (spread) {
+      // V elements that are not finite, for the rows that see their key (from the pool:
+      // the copy in LDS is the next block's by now)
+#pragma unroll 1
+      for (int kk = 0; kk < kBK; ++kk) {
+        const int kh = kk >> 4, j = j0 + kk;
+        if (cur[kh] < 0 || j >= tail_r.hi) continue;
+        const __bf16* vr = reinterpret_cast<const __bf16*>(vp + half_offset(cur[kh], j));
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          uint32_t w = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w = e == (kk >> 1 & 1) + 2 * kh ? pk[x][e] : w;
+          const uint32_t pw = uint32_t(__shfl(int(w), l16 + 16 * ((kk & 15) >> 2)));
+          const float p = __uint_as_float((kk & 1) ? pw & 0xffff0000u : pw << 16);
+          const bool seen = j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
+#pragma unroll
+          for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = float(vr[16 * dt + 4 * grp + e]);
+              if (seen && !isfinite(v)) o[dt][x][e] += p * v;
+            }
+        }
+      }
+    }
+    tb = next;
+  }
+
+  // join the waves (over the K and V blocks, once all are read)
+  __syncthreads();
+  float* part = reinterpret_cast<float*>(lds);
+  float* part_m = part + kWaves * C::kRows * C::kPitch;
+  float* part_l = part_m + kWaves * C::kRows;
+  float* part_u = part_l + kWaves * C::kRows;
+#pragma unroll
+  for (int x = 0; x < QT; ++x) {
+    const int row = wave * C::kRows + 16 * x + l16;
+    const float u = sum_across_groups(l_run[x]);
+    if (grp == 0) {
+      part_m[row] = m_run[x];
+      part_l[row] = lsum[x][0];
+      part_u[row] = u;
+    }
+#pragma unroll
+    for (int dt = 0; dt < C::DT; ++dt)
+      *reinterpret_cast<f32x4*>(part + row * C::kPitch + 16 * dt + 4 * grp) = o[dt][x];
+  }
+  __syncthreads();
+  float* ws = t.part + (int64_t(item) * b.kv_heads + head) * paged_part_floats(C::kRows, D);
+  for (int n = threadIdx.x; n < C::kRows * (D / 8); n += kThreads) {
+    const int r = n / (D / 8), c = n % (D / 8);
+    if (row0 + r > row1) continue;
+    float m = part_m[r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w * C::kRows + r]);
+    float l = 0.0f, u = 0.0f;
+    f32x4 acc[2] = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int row = w * C::kRows + r;
+      const float a = __builtin_amdgcn_exp2f(part_m[row] - m);
+      l += a * part_l[row];
+      u += a * part_u[row];
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        acc[x] += a * *reinterpret_cast<const f32x4*>(part + row * C::kPitch + 8 * c + 4 * x);
+    }
+    if (it.parts > 1) {
+      *reinterpret_cast<f32x4*>(ws + r * D + 8 * c) = acc[0];
+      *reinterpret_cast<f32x4*>(ws + r * D + 8 * c + 4) = acc[1];
+      if (c == 0) {
+        ws[C::kRows * D + r] = m;
+        ws[C::kRows * D + C::kRows + r] = l;
+        ws[C::kRows * D + 2 * C::kRows + r] = u;
+      }
+    } else {
+      const int tau = (row0 + r) / b.group;
+      const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
+                         (row0 + r - tau * b.group);
+      paged_store<__bf16, 8>(static_cast<__bf16*>(t.out) + at * D + 8 * c,
+                             reinterpret_cast<const float*>(acc), l);
+      if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m, u);
+    }
+  }
+}
+
+template <int D, int QT>
+hipError_t launch(const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t, int64_t items,
+                  hipStream_t stream) {
+  hipLaunchKernelGGL((paged_attn_kernel<D, QT>), dim3(unsigned(items * b.kv_heads)), dim3(kThreads),
+                     0, stream, b, sp, t);
+  return hipGetLastError();
+}
+
+// Joins the parts of the tiles that have several: workgroup (tile, kv head), thread
+// (row, 4 elements of d) after thread.
+template <class T, int D, int RT, int KB>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedBatch b, PagedSplit sp, PagedTensors t,
+                                                         int max_items) {
+  const int lane = threadIdx.x & 63;
+  const int head = blockIdx.x % b.kv_heads;
+  PagedItem it;
+  if (!PagedScan<RT, KB>::find(b, sp, blockIdx.x / b.kv_heads, true, lane, &it)) return;
+  if (it.parts <= 1 || it.item0 + it.parts > max_items) return;
+  const int n_rows = min(it.seq.n_new * b.group - it.tile * RT, RT);
+  const int64_t stride = paged_part_floats(RT, D);
+  const float* p0 = t.part + (int64_t(it.item0) * b.kv_heads + head) * stride;
+  const int64_t step = stride * b.kv_heads;   // from part to part
+  // (references are in log2 units in the bf16 kernel, in natural units in the float32 one)
+  constexpr float kUnit = sizeof(T) == 2 ? 1.0f : 1.44269504f;
+  for (int n = threadIdx.x; n < n_rows * (D / 4); n += 256) {
+    const int r = n / (D / 4), c = n % (D / 4);
+    float m = -FLT_MAX;
+    for (int p = 0; p < it.parts; ++p) m = fmaxf(m, p0[p * step + RT * D + r]);
+    float l = 0.0f, u = 0.0f;
+    f32x4 acc = {};
+    for (int p = 0; p < it.parts; ++p) {
+      const float* pp = p0 + p * step;
+      const float a = __builtin_amdgcn_exp2f((pp[RT * D + r] - m) * kUnit);
+      l += a * pp[RT * D + RT + r];
+      u += a * pp[RT * D + 2 * RT + r];
+      acc += a * *reinterpret_cast<const f32x4*>(pp + r * D + 4 * c);
+    }
+    const int row = it.tile * RT + r, tau = row / b.group;
+    const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
+                       (row - tau * b.group);
+    paged_store<T, 4>(static_cast<T*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc), l);
+    if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m * kUnit, u);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_paged_attn_bf16(int qt, const PagedBatch& b, const PagedSplit& sp,
+                                  const PagedTensors& t, int64_t items, int head_dim,
+                                  hipStream_t stream) {
+  if (head_dim == 64) return qt == 2 ? launch<64, 2>(b, sp, t, items, stream) : launch<64, 1>(b, sp, t, items, stream);
+  return qt == 2 ? launch<128, 2>(b, sp, t, items, stream) : launch<128, 1>(b, sp, t, items, stream);
+}
+
+hipError_t launch_paged_join(int qt, const PagedBatch& b, const PagedSplit& sp,
+                             const PagedTensors& t, int64_t items, int64_t tiles, int head_dim,
+                             int dtype, hipStream_t stream) {
+  const dim3 grid(unsigned(tiles * b.kv_heads));
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, b, sp, t, int(items));
+    return hipGetLastError();
+  };
+  if (dtype == FF_DT_BF16) {
+    if (head_dim == 64)
+      return qt == 2 ? go(paged_join_kernel<__bf16, 64, 32, 32>) : go(paged_join_kernel<__bf16, 64, 16, 32>);
+    return qt == 2 ? go(paged_join_kernel<__bf16, 128, 32, 32>) : go(paged_join_kernel<__bf16, 128, 16, 32>);
+  }
+  if (head_dim == 64)
+    return qt == 2 ? go(paged_join_kernel<float, 64, 32, 16>) : go(paged_join_kernel<float, 64, 16, 16>);
+  return qt == 2 ? go(paged_join_kernel<float, 128, 32, 16>) : go(paged_join_kernel<float, 128, 16, 16>);
+}
+
+}  // namespace ff

@@ -46,31 +46,6 @@ __device__ inline void store_nt(uint4 x, uint4* p) {
   __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
 }
 
-__device__ inline uint32_t rotate_bf16_pair(uint32_t w, double2 cs) {
-  const double a = bf16_lo(w), b = bf16_hi(w);
-  const double o0 = a * cs.x - b * cs.y;
-  const double o1 = a * cs.y + b * cs.x;
-  return pack_bf16_rne(round_to_odd_f32(o0), round_to_odd_f32(o1));
-}
-
-template <typename T>
-__device__ inline uint4 rotate_vec(uint4 w, const double2* cs) {
-  if constexpr (sizeof(T) == 2) {
-    w.x = rotate_bf16_pair(w.x, cs[0]);
-    w.y = rotate_bf16_pair(w.y, cs[1]);
-    w.z = rotate_bf16_pair(w.z, cs[2]);
-    w.w = rotate_bf16_pair(w.w, cs[3]);
-  } else {
-    const double a0 = __uint_as_float(w.x), b0 = __uint_as_float(w.y);
-    const double a1 = __uint_as_float(w.z), b1 = __uint_as_float(w.w);
-    w.x = __float_as_uint(float(a0 * cs[0].x - b0 * cs[0].y));
-    w.y = __float_as_uint(float(a0 * cs[0].y + b0 * cs[0].x));
-    w.z = __float_as_uint(float(a1 * cs[1].x - b1 * cs[1].y));
-    w.w = __float_as_uint(float(a1 * cs[1].y + b1 * cs[1].x));
-  }
-  return w;
-}
-
 // Rotation of the block's vectors of Q (when HQ) and K, of which the first U per
 // thread are in bq and bk: the steady loop has no per-lane branch (every lane
 // holds a vector), the next vectors loaded before the current ones are rotated

@@ -1,4 +1,4 @@
-"""Thin Python binding of libff (include/ff.h) over ctypes.
+"""Thin Python binding of libff (include/ff.h, include/ff_paged.h) over ctypes.
 
 Argument marshalling only: every step runs in the HIP library.  PyTorch is
 used for device memory (the cache buffer, tensors) and for the current HIP
@@ -7,6 +7,7 @@ loading fails loudly otherwise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -26,6 +27,7 @@ MAX_ANCHOR_FRAMES = 8
 MAX_ROPE_FRAMES = 16
 MAX_PACKED_CHUNKS = 128
 MAX_BATCH = 4
+MAX_PAGED_SEQS = 1024
 ABI_VERSION = 4
 
 
@@ -67,6 +69,27 @@ class AttentionItem(ctypes.Structure):
         ("out", ctypes.c_void_p), ("bank_k", ctypes.c_void_p), ("bank_v", ctypes.c_void_p),
         ("n_frames", ctypes.c_int32), ("reserved", ctypes.c_int32),
         ("frame_index", ctypes.POINTER(ctypes.c_int32)),
+    ]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [
+        ("num_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+        ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("min_new", ctypes.c_int32),
+        ("max_new", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("table_stride", ctypes.c_int64), ("q_start", ctypes.c_void_p),
+        ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+    ]
+
+
+class PagedRope(ctypes.Structure):
+    _fields_ = [
+        ("rope_pairs_t", ctypes.c_int32), ("rope_pairs_h", ctypes.c_int32),
+        ("rope_pairs_w", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("rope_theta", ctypes.c_double),
     ]
 
 
@@ -116,6 +139,15 @@ SIGNATURES = [
     ("ff_last_error", ctypes.c_char_p, []),
 ]
 
+# the same of include/ff_paged.h
+PAGED_SIGNATURES = [
+    ("ff_paged_append", _I32, [ctypes.POINTER(PagedDesc), ctypes.POINTER(PagedRope), _VP, _VP, _VP,
+                               _I64, _I64, _I64, _VP, _VP, _VP, _VP, _VP]),
+    ("ff_paged_attention_workspace", _SZ, [ctypes.POINTER(PagedDesc)]),
+    ("ff_paged_attention", _I32, [ctypes.POINTER(PagedDesc), _VP, _I64, _VP, _VP, _VP, _VP,
+                                  ctypes.c_float, _I32, _I32, _I32, _VP, _SZ, _VP]),
+]
+
 _lib = None
 
 
@@ -127,7 +159,7 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2609_32540_amd.build` (the HIP path has no fallback)")
         L = ctypes.CDLL(LIB_PATH)
-        for name, res, args in SIGNATURES:
+        for name, res, args in SIGNATURES + PAGED_SIGNATURES:
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args
@@ -537,6 +569,166 @@ def packed_attention_bwd_static(q, k, v, out, dout, lse, dq, dk, dv, d_anchor_k=
     _check(lib().ff_packed_attention_bwd_static(
         ctypes.byref(desc), ptrs[0], ptrs[1], ptrs[2], akp, avp, ptrs[3], ptrs[4], lp,
         ptrs[5], ptrs[6], ptrs[7], dak, dav, scale, _stream_handle(dev, stream)))
+
+
+# ----------------------------------------------------------------------
+def _int32_on(t: torch.Tensor, device: torch.device, name: str) -> int:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != torch.int32 or t.device != device:
+        raise ValueError(f"{name} must be int32 on {device} (got {t.dtype} on {t.device})")
+    return t.data_ptr()
+
+
+def _paged_desc(q_heads: int, n_tokens: int, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
+                min_new: int, max_new: int) -> PagedDesc:
+    dev, dt = k_pages.device, k_pages.dtype
+    if dt not in (torch.bfloat16, torch.float32):
+        raise ValueError("dtype must be torch.bfloat16 or torch.float32")
+    if k_pages.dim() != 4:
+        raise ValueError("k_pages must be [num_pages][kv heads][page tokens][d]")
+    _dense(k_pages, k_pages.shape, dt, dev, "k_pages")
+    _dense(v_pages, k_pages.shape, dt, dev, "v_pages")
+    n_seqs = kv_len.shape[0] if kv_len.dim() == 1 else -1
+    if n_seqs < 0 or q_start.shape != (n_seqs + 1,) or page_table.dim() != 2 or page_table.shape[0] != n_seqs:
+        raise ValueError("kv_len must be [n_seqs], q_start [n_seqs + 1], page_table [n_seqs][max_pages]")
+    if not kv_len.is_contiguous() or not q_start.is_contiguous():
+        raise ValueError("kv_len and q_start must be contiguous")
+    max_pages = page_table.shape[1]
+    stride = page_table.stride(0) if n_seqs > 1 else max_pages
+    if max_pages > 1 and page_table.stride(1) != 1:
+        raise ValueError("the rows of page_table must be contiguous")
+    return PagedDesc(k_pages.shape[0], k_pages.shape[2], q_heads, k_pages.shape[1], k_pages.shape[3],
+                     FF_DT_BF16 if dt == torch.bfloat16 else FF_DT_F32, n_seqs, n_tokens, max_pages,
+                     min_new, max_new, 0, stride, _int32_on(q_start, dev, "q_start"),
+                     _int32_on(kv_len, dev, "kv_len"), _int32_on(page_table, dev, "page_table"))
+
+
+def _rows(t: torch.Tensor, like: torch.Tensor, name: str) -> Tuple[int, int]:
+    """(pointer, elements between rows) of [n_tokens][heads][d] rows of heads, each dense."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device != like.device or t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype} on {like.device} (got {t.dtype} on {t.device})")
+    d = like.shape[3]
+    if t.dim() != 3 or t.shape[2] != d:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [n_tokens][heads][{d}]")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d):
+        raise ValueError(f"the heads of a row of {name} must be contiguous")
+    # (a single row may report any stride)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * d
+
+
+def _on_device(device: torch.device):
+    """The tensors' device as the current one, which a launch needs."""
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def paged_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                 q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, *,
+                 q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 positions: Optional[torch.Tensor] = None,
+                 rope_pairs: Optional[Tuple[int, int, int]] = None, rope_theta: float = 10000.0,
+                 stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
+    """ff_paged_append: rotate K (and Q) of the new tokens, write K and V to the pages.
+
+    k, v: [n_tokens][kv heads][d] (rows may be slices of wider ones); k_pages, v_pages:
+    [num_pages][kv heads][page tokens][d]; q_start [n_seqs + 1], kv_len [n_seqs] (new tokens
+    included) and page_table [n_seqs][max_pages] are int32 on the device.  positions (optional,
+    int32 [n_tokens][3]): t, h, w of each row, default the token's index on every axis.
+    Returns the rotated q (q_out, or a new tensor whose rows of no token are undefined),
+    None without q.
+    """
+    if k.shape != v.shape:
+        raise ValueError("k and v must have one shape")
+    n = k.shape[0]
+    dev = k_pages.device
+    desc = _paged_desc(q.shape[1] if q is not None and q.dim() == 3 else k_pages.shape[1], n, k_pages,
+                       v_pages, q_start, kv_len, page_table, 0, 0)
+    kp, ks = _rows(k, k_pages, "k")
+    vp, vs = _rows(v, k_pages, "v")
+    if k.shape[1] != k_pages.shape[1]:
+        raise ValueError(f"k has {k.shape[1]} heads, the pool {k_pages.shape[1]}")
+    qp = qop = None
+    qs = 0
+    if q is not None:
+        qp, qs = _rows(q, k_pages, "q")
+        if q.shape[0] != n:
+            raise ValueError(f"q has {q.shape[0]} rows, k {n}")
+        if q_out is None:
+            q_out = _empty_on(q, stream)
+        qop = _dense(q_out, q.shape, q.dtype, dev, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    pp = None
+    if positions is not None:
+        if positions.shape != (n, 3) or not positions.is_contiguous():
+            raise ValueError(f"positions must be a contiguous [{n}][3] tensor")
+        pp = _int32_on(positions, dev, "positions")
+    rp = rope_pairs if rope_pairs is not None else (0, 0, 0)
+    rope = PagedRope(rp[0], rp[1], rp[2], 0, rope_theta)
+    with _on_device(dev):
+        _check(lib().ff_paged_append(ctypes.byref(desc), ctypes.byref(rope), qp, kp, vp, qs, ks, vs, pp,
+                                     qop, k_pages.data_ptr(), v_pages.data_ptr(),
+                                     _stream_handle(dev, stream)))
+    return q_out
+
+
+def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                    q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor, *,
+                    block: bool = False, window: int = -1, anchor_tokens: int = 0,
+                    min_new: int = 0, max_new: int = 0, scale: Optional[float] = None,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None,
+                    stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """ff_paged_attention: attention of the new tokens over their sequences' pages.
+
+    q: [n_tokens][q heads][d] (rotated; rows may be slices of wider ones); the pool and the
+    batch as in paged_append.  block: the new tokens see each other; window, anchor_tokens:
+    which earlier tokens are seen.  min_new, max_new: bounds of a sequence's new tokens if
+    known (they choose kernels).  lse (optional, float32 [n_tokens][q heads]) receives the
+    base-2 log-sum-exp.  Rows of no sequence keep what `out` holds (a new `out`: undefined).
+    workspace: a uint8 tensor of paged_attention_workspace() bytes, default a new one.
+    """
+    desc = _paged_desc(q.shape[1] if q.dim() == 3 else 0, q.shape[0], k_pages, v_pages, q_start, kv_len,
+                       page_table, min_new, max_new)
+    dev = k_pages.device
+    qp, qs = _rows(q, k_pages, "q")
+    if out is None:
+        out = _empty_on(q, stream)
+    op = _dense(out, q.shape, q.dtype, dev, "out")
+    lp = _dense(lse, q.shape[:2], torch.float32, dev, "lse") if lse is not None else None
+    if scale is None:
+        scale = 1.0 / math.sqrt(q.shape[2])
+    with _on_device(dev):
+        wp, wn = None, 0
+        if workspace is not None:
+            if workspace.device != dev or not workspace.is_contiguous():
+                raise ValueError("workspace must be a contiguous tensor on the pool's device")
+            wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        else:
+            wn = lib().ff_paged_attention_workspace(ctypes.byref(desc))
+            if wn:
+                workspace = _bytes_on(wn, dev, stream)
+                wp = workspace.data_ptr()
+        _check(lib().ff_paged_attention(ctypes.byref(desc), qp, qs, k_pages.data_ptr(), v_pages.data_ptr(),
+                                        op, lp, scale, int(block), window, anchor_tokens, wp, wn,
+                                        _stream_handle(dev, stream)))
+    return out
+
+
+def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, q_start: torch.Tensor,
+                              kv_len: torch.Tensor, page_table: torch.Tensor, *, min_new: int = 0,
+                              max_new: int = 0) -> int:
+    """ff_paged_attention_workspace: workspace bytes of a paged_attention call (sizes only)."""
+    desc = _paged_desc(q.shape[1], q.shape[0], k_pages, k_pages, q_start, kv_len, page_table, min_new,
+                       max_new)
+    with _on_device(k_pages.device):
+        n = lib().ff_paged_attention_workspace(ctypes.byref(desc))
+    if n == 0 and lib().ff_last_error():
+        raise FFError(1, lib().ff_last_error().decode())
+    return n
 
 
 def anchor_partition(L: int, delta: int) -> List[int]:

@@ -1,0 +1,166 @@
+"""The paged cache's host side without a GPU: exported symbols, refusals (only calls that never
+reach a launch; the fake device pointers are never dereferenced), workspace sizes, and the
+float64 reference of the GPU tests against the repository's oracle."""
+import ctypes
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ff_oracle as fo
+from paper_2609_32540_amd import ff
+
+import paged_ref as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+DEV = 0x7f0000000000     # aligned; never dereferenced here
+
+
+def test_library_exports_every_header_symbol():
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "ff_paged.h")).read(), flags=re.S)
+    names = set(re.findall(r"\b(ff_[a-z0-9_]+)\s*\(", text))
+    assert names == {n for n, _, _ in ff.PAGED_SIGNATURES} and len(names) == 3
+    for n in names:
+        assert hasattr(ff.lib(), n)
+
+
+def desc(**kw):
+    base = dict(num_pages=100, page_tokens=16, num_q_heads=8, num_kv_heads=2, head_dim=128,
+                dtype=ff.FF_DT_BF16, n_seqs=3, n_tokens=3, max_pages=10, min_new=0, max_new=1, reserved=0,
+                table_stride=10, q_start=DEV, kv_len=DEV, page_table=DEV)
+    base.update(kw)
+    return ff.PagedDesc(**base)
+
+
+def append(d, q=DEV, k=DEV, v=DEV, qs=1024, ks=256, vs=256, pos=None, q_out=DEV, kp=DEV, vp=DEV,
+           rope=(0, 0, 0), theta=10000.0):
+    r = ff.PagedRope(*rope, 0, theta)
+    return ff.lib().ff_paged_append(ctypes.byref(d), ctypes.byref(r), q, k, v, qs, ks, vs, pos, q_out, kp, vp, None)
+
+
+def attend(d, q=DEV, qs=1024, kp=DEV, vp=DEV, out=DEV, lse=None, scale=0.1, block=0, window=-1, anchors=0,
+           ws=DEV, wn=1 << 40):
+    return ff.lib().ff_paged_attention(ctypes.byref(d), q, qs, kp, vp, out, lse, scale, block, window, anchors,
+                                       ws, wn, None)
+
+
+BAD_DESC = [("num_pages", 0, 1), ("page_tokens", 8, 5), ("page_tokens", 48, 5), ("page_tokens", 512, 5),
+            ("page_tokens", 0, 5), ("num_kv_heads", 0, 1), ("num_q_heads", 0, 1), ("num_q_heads", 7, 2),
+            ("num_q_heads", 2 ** 30, 5), ("head_dim", 96, 5), ("dtype", 2, 5), ("n_seqs", -1, 5),
+            ("n_seqs", 1025, 5), ("n_tokens", -1, 1), ("n_tokens", 2 ** 31 - 1, 5), ("min_new", -1, 1),
+            ("max_new", -2, 1), ("min_new", 2, 1), ("max_pages", 0, 1), ("max_pages", 2 ** 27, 5),
+            ("table_stride", 9, 2), ("q_start", None, 1), ("kv_len", None, 1), ("page_table", None, 1),
+            ("q_start", DEV + 2, 1), ("kv_len", DEV + 1, 1), ("page_table", DEV + 2, 1)]
+
+
+@pytest.mark.parametrize("field,value,status", BAD_DESC)
+def test_invalid_desc_is_refused(field, value, status):
+    d = desc(**{field: value})
+    if field == "max_pages" and value > 10:
+        d.table_stride = value
+    assert append(d) == status
+    assert ff.lib().ff_last_error()
+    assert attend(d) == status
+    assert ff.lib().ff_paged_attention_workspace(ctypes.byref(d)) == 0 and ff.lib().ff_last_error()
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(k=None), 1), (dict(v=None), 1), (dict(q_out=None), 1), (dict(kp=None), 1), (dict(vp=None), 1),
+    (dict(q=DEV + 8), 1), (dict(k=DEV + 2), 1), (dict(v=DEV + 4), 1), (dict(q_out=DEV + 8), 1),
+    (dict(kp=DEV + 8), 1), (dict(vp=DEV + 8), 1), (dict(pos=DEV + 1), 1), (dict(qs=1016), 2), (dict(ks=248), 2),
+    (dict(vs=255), 2), (dict(ks=260), 2), (dict(qs=2 ** 31 + 8), 2), (dict(qs=2048), 2),
+    (dict(rope=(64, 1, 0)), 1), (dict(rope=(-1, 65, 0)), 1), (dict(theta=0.0), 1), (dict(theta=math.nan), 1),
+    (dict(theta=math.inf), 1)])
+def test_append_refusals(kw, status):
+    """(qs=2048 with q_out == q: in place needs dense rows)"""
+    assert append(desc(), **kw) == status
+    assert ff.lib().ff_last_error()
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=None), 1), (dict(out=None), 1), (dict(kp=None), 1), (dict(vp=None), 1), (dict(q=DEV + 8), 1),
+    (dict(out=DEV + 8), 1), (dict(kp=DEV + 8), 1), (dict(vp=DEV + 8), 1), (dict(lse=DEV + 2), 1),
+    (dict(ws=DEV + 8), 1), (dict(qs=1016), 2), (dict(qs=1030), 2), (dict(scale=0.0), 1), (dict(scale=-1.0), 1),
+    (dict(scale=math.nan), 1), (dict(scale=math.inf), 1), (dict(block=2), 1), (dict(window=-2), 1),
+    (dict(anchors=-1), 1)])
+def test_attention_refusals(kw, status):
+    assert attend(desc(), **kw) == status
+    assert ff.lib().ff_last_error()
+
+
+def test_workspace():
+    L = ff.lib()
+    assert L.ff_paged_attention_workspace(ctypes.byref(desc(max_pages=10))) == 0
+    long = desc(max_pages=4096, table_stride=4096)
+    n = L.ff_paged_attention_workspace(ctypes.byref(long))
+    assert n > 0
+    assert attend(long, ws=None) == 1
+    assert attend(long, wn=n - 1) == 7
+    # it follows from sizes alone
+    assert n == L.ff_paged_attention_workspace(ctypes.byref(desc(max_pages=4096, table_stride=5000, q_start=DEV + 64)))
+    # and stays moderate where the batch and the cache are large
+    most = desc(max_pages=8192, table_stride=8192, n_seqs=1024, n_tokens=1024, num_q_heads=64, num_kv_heads=8)
+    assert L.ff_paged_attention_workspace(ctypes.byref(most)) < 2 ** 28
+
+
+def test_nothing_to_do_is_ok():
+    for kw in (dict(n_seqs=0, q_start=None, kv_len=None, page_table=None), dict(n_tokens=0)):
+        assert append(desc(**kw), k=None, v=None, q=None) == 0
+        assert attend(desc(**kw), q=None, out=None) == 0
+    assert not ff.lib().ff_last_error()
+
+
+def test_binding_refusals():
+    i32 = dict(dtype=torch.int32)
+    kp = torch.zeros((4, 2, 16, 128), dtype=torch.bfloat16)
+    good = dict(q_start=torch.tensor([0, 1], **i32), kv_len=torch.tensor([5], **i32), page_table=torch.zeros((1, 2), **i32))
+    q = torch.zeros((1, 8, 128), dtype=torch.bfloat16)
+    k = torch.zeros((1, 2, 128), dtype=torch.bfloat16)
+
+    def att(q=q, kp=kp, vp=kp, **kw):
+        b = dict(good, **{n: kw.pop(n) for n in list(kw) if n in good})
+        ff.paged_attention(q, kp, vp, b["q_start"], b["kv_len"], b["page_table"], **kw)
+
+    def app(k=k, v=k, kp=kp, **kw):
+        ff.paged_append(k, v, kp, kp, good["q_start"], good["kv_len"], good["page_table"], **kw)
+
+    for bad in (dict(kp=kp.half()), dict(kp=kp[0]), dict(vp=kp[:2]), dict(kp=kp[:, :, :, :64]),
+                dict(kv_len=good["kv_len"].long()), dict(q_start=torch.tensor([0], **i32)),
+                dict(page_table=torch.zeros((2, 2), **i32)), dict(page_table=torch.zeros((1, 4), **i32)[:, ::2]),
+                dict(q=q.float()), dict(q=q[0]), dict(q=torch.zeros((1, 8, 64), dtype=torch.bfloat16)),
+                dict(q=torch.zeros((1, 8, 256), dtype=torch.bfloat16)[:, :, ::2]), dict(out=q.float()),
+                dict(out=torch.zeros((2, 8, 128), dtype=torch.bfloat16)), dict(lse=torch.zeros((1, 8))[:, ::2])):
+        with pytest.raises((ValueError, TypeError)):
+            att(**bad)
+    for bad in (dict(v=k.float()), dict(k=k.repeat(2, 1, 1)), dict(k=k.repeat(1, 2, 1), v=k.repeat(1, 2, 1)),
+                dict(q=q.repeat(2, 1, 1)), dict(q_out=q), dict(q=q, q_out=q.float()),
+                dict(positions=torch.zeros((1, 3))), dict(positions=torch.zeros((1, 2), **i32))):
+        with pytest.raises((ValueError, TypeError)):
+            app(**bad)
+
+
+def test_reference_against_the_oracle():
+    """One sequence whose pages are in order: causal and block attention, and the rotation."""
+    rng = np.random.default_rng(1)
+    n, d, page = 24, 64, 16
+    k, v, q = (rng.standard_normal((n, 1, d)) for _ in range(3))
+    kp, vp = (torch.zeros((2, 1, page, d), dtype=torch.float64) for _ in range(2))
+    table = torch.tensor([[1, 0]], dtype=torch.int32)
+    for pool, x in ((kp, k), (vp, v)):
+        pool[1, :, :], pool[0, :, :8] = torch.tensor(x[:16]).transpose(0, 1), torch.tensor(x[16:]).transpose(0, 1)
+    b = ref.Batch([0, 10], [n], table, page, 2)
+    mine = ref.attention(b, torch.tensor(q[-10:]).float(), kp, vp)
+    for row in range(10):
+        sc = k[:15 + row, 0] @ q[14 + row, 0].astype(np.float32).astype(np.float64) / 8.0
+        p = np.exp(sc - sc.max())
+        assert np.allclose(mine.out[row, 0], p @ v[:15 + row, 0] / p.sum(), atol=1e-12)
+    blocks = ref.attention(b, torch.tensor(q[-10:]).float(), kp, vp, block=True)
+    want = fo.attend(q[-10:, 0].astype(np.float32).astype(np.float64), k[:, 0], v[:, 0], 1.0 / 8.0)
+    assert np.allclose(blocks.out[:, 0], want, atol=1e-12)
+    x = rng.standard_normal((6, 1, d))
+    want = fo.rope3d(x, [3], 2, 3, fo.rope_pair_split(d), 10000.0)
+    for t in range(6):
+        assert np.allclose(ref.rotate(x[t], [3, t // 3, t % 3], ref.rope_split(d), 10000.0), want[t], atol=1e-12)
