@@ -101,31 +101,75 @@ ff::PagedBatch make_batch(const ff_paged_desc& d) {
 
 // Launch choices of one attention call: they follow from sizes, so that the workspace can
 // be asked for ahead of it.
-struct Plan {
-  int qt;            // 16-row query tiles per workgroup
+struct Launch {
+  int rows;              // of a tile: 16, 32 or kPagedPromptRows; 0: no launch
   ff::PagedSplit split;
-  int64_t tiles;     // at most this many tiles per kv head
-  int64_t items;     // and items
-  size_t workspace;
+  int64_t tiles, items;  // at most this many per kv head
+  size_t part_bytes;     // of its partial results
 };
+struct Plan {
+  Launch few, many;      // sequences of few rows, and of many
+};
+
+// Rows (new tokens x query heads per kv head) from which a sequence goes to the kernel of
+// 256-row tiles.
+constexpr int kManyRows = 64;
+
+void set_items(const ff_paged_desc& d, Launch* l, int64_t blocks) {
+  if (blocks <= l->split.min_per) l->split.target = 0;
+  l->items = ff::paged_max_items(l->tiles, l->split);
+  l->part_bytes = l->split.target > 0 ? size_t(l->items) * d.num_kv_heads *
+                                            ff::paged_part_floats(l->rows, d.head_dim) * 4 : 0;
+}
 
 Plan make_plan(const ff_paged_desc& d) {
   Plan p;
-  const int group = d.num_q_heads / d.num_kv_heads;
-  const int64_t most = d.max_new > 0 ? std::min(d.max_new, d.n_tokens) : d.n_tokens;
-  p.qt = most * group <= 16 ? 1 : 2;
-  const int block = d.dtype == FF_DT_BF16 ? 32 : 16;
-  const int64_t blocks = (int64_t(d.max_pages) * d.page_tokens + block - 1) / block;
-  p.split.min_per = 256 / block;
-  p.split.target = blocks > p.split.min_per
-                       ? (4 * ff::device_cus() + d.num_kv_heads - 1) / d.num_kv_heads : 0;
-  p.split.min_rows = 0;
-  p.split.max_rows = INT32_MAX;
-  p.tiles = ff::paged_max_items(d.n_tokens, d.n_seqs, group, 16 * p.qt, 0);
-  p.items = ff::paged_max_items(d.n_tokens, d.n_seqs, group, 16 * p.qt, p.split.target);
-  p.workspace = p.split.target > 0 ? size_t(p.items) * d.num_kv_heads *
-                                         ff::paged_part_floats(16 * p.qt, d.head_dim) * 4 : 0;
+  std::memset(&p, 0, sizeof(p));
+  const int group = d.num_q_heads / d.num_kv_heads, cus = ff::device_cus();
+  const int64_t rows = int64_t(d.n_tokens) * group;
+  const int64_t most = (d.max_new > 0 ? std::min(d.max_new, d.n_tokens) : d.n_tokens) * int64_t(group);
+  const int64_t keys = int64_t(d.max_pages) * d.page_tokens;
+  const bool bf16 = d.dtype == FF_DT_BF16;
+  const bool many = bf16 && most > kManyRows, few = !many || int64_t(d.min_new) * group <= kManyRows;
+  if (few) {
+    Launch& l = p.few;
+    l.rows = most <= 16 ? 16 : 32;
+    l.split.min_rows = 0;
+    l.split.max_rows = many ? kManyRows : INT32_MAX;
+    l.tiles = (rows + l.rows - 1) / l.rows + d.n_seqs;
+    if (many) l.tiles = std::min(l.tiles, int64_t(d.n_seqs) * ((kManyRows + l.rows - 1) / l.rows));
+    const int block = bf16 ? 32 : 16;
+    l.split.min_per = 256 / block;
+    l.split.target = (2 * cus + d.num_kv_heads - 1) / d.num_kv_heads;
+    l.split.spread = l.tiles * d.num_kv_heads <= 16 * cus ? 2 : 0;
+    set_items(d, &l, (keys + block - 1) / block);
+  }
+  if (many) {
+    Launch& l = p.many;
+    l.rows = ff::kPagedPromptRows;
+    l.split.min_rows = few ? kManyRows : 0;
+    l.split.max_rows = INT32_MAX;
+    l.tiles = (rows + l.rows - 1) / l.rows + (few ? std::min(int64_t(d.n_seqs), rows / kManyRows) : d.n_seqs);
+    l.split.min_per = 8;
+    l.split.target = std::max(cus / d.num_kv_heads, 1);
+    l.split.spread = 0;
+    set_items(d, &l, (keys + 63) / 64);
+  }
   return p;
+}
+
+hipError_t run(const Launch& l, const ff_paged_desc& d, const ff::PagedBatch& b,
+               const ff::PagedTensors& t, hipStream_t stream) {
+  hipError_t e;
+  if (l.rows == ff::kPagedPromptRows)
+    e = ff::launch_paged_prompt(b, l.split, t, l.items, d.head_dim, stream);
+  else if (d.dtype == FF_DT_BF16)
+    e = ff::launch_paged_attn_bf16(l.rows / 16, b, l.split, t, l.items, d.head_dim, stream);
+  else
+    e = ff::launch_paged_attn_f32(l.rows / 16, b, l.split, t, l.items, d.head_dim, stream);
+  if (e == hipSuccess && l.split.target > 0)
+    e = ff::launch_paged_join(l.rows, b, l.split, t, l.items, l.tiles, d.head_dim, d.dtype, stream);
+  return e;
 }
 
 }  // namespace
@@ -184,7 +228,8 @@ ff_status ff_paged_append(const ff_paged_desc* desc, const ff_paged_rope* rope, 
 size_t ff_paged_attention_workspace(const ff_paged_desc* desc) {
   if (check_desc(desc) != FF_OK) return 0;
   ok();
-  return make_plan(*desc).workspace;
+  const Plan p = make_plan(*desc);
+  return p.few.part_bytes + p.many.part_bytes;
 }
 
 ff_status ff_paged_attention(const ff_paged_desc* desc, const void* q, int64_t q_stride,
@@ -209,11 +254,12 @@ ff_status ff_paged_attention(const ff_paged_desc* desc, const void* q, int64_t q
       check_aligned(workspace, 16, "workspace") != FF_OK)
     return FF_ERR_INVALID_ARG;
   const Plan p = make_plan(d);
-  if (p.workspace > 0 && !workspace) return fail(FF_ERR_INVALID_ARG, "workspace is NULL");
-  if (workspace_bytes < p.workspace)
-    return fail(FF_ERR_BUFFER, "workspace_bytes %zu < required %zu", workspace_bytes, p.workspace);
+  const size_t need = p.few.part_bytes + p.many.part_bytes;
+  if (need > 0 && !workspace) return fail(FF_ERR_INVALID_ARG, "workspace is NULL");
+  if (workspace_bytes < need)
+    return fail(FF_ERR_BUFFER, "workspace_bytes %zu < required %zu", workspace_bytes, need);
   // (a grid holds at most 2^32 - 1 threads)
-  if (p.items * d.num_kv_heads > int64_t(UINT32_MAX) / 512)
+  if (std::max(p.few.items, p.many.items) * d.num_kv_heads > int64_t(UINT32_MAX) / 512)
     return fail(FF_ERR_UNSUPPORTED, "too many rows for one launch");
   ff::PagedBatch b = make_batch(d);
   b.window = std::min(window, 1 << 30);
@@ -231,11 +277,10 @@ ff_status ff_paged_attention(const ff_paged_desc* desc, const void* q, int64_t q
   t.scale = softmax_scale;
   t.scale_log2 = float(double(softmax_scale) * 1.4426950408889634);
   const hipStream_t hs = static_cast<hipStream_t>(stream);
-  hipError_t e = d.dtype == FF_DT_BF16
-                     ? ff::launch_paged_attn_bf16(p.qt, b, p.split, t, p.items, d.head_dim, hs)
-                     : ff::launch_paged_attn_f32(p.qt, b, p.split, t, p.items, d.head_dim, hs);
-  if (e == hipSuccess && p.split.target > 0)
-    e = ff::launch_paged_join(p.qt, b, p.split, t, p.items, p.tiles, d.head_dim, d.dtype, hs);
+  hipError_t e = hipSuccess;
+  if (p.few.rows > 0) e = run(p.few, d, b, t, hs);
+  t.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.few.part_bytes);
+  if (e == hipSuccess && p.many.rows > 0) e = run(p.many, d, b, t, hs);
   return hip_status(e, "paged_attention launch");
 }
 

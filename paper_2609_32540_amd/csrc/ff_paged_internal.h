@@ -39,6 +39,18 @@ struct PagedAppend {
   double omega[64];         // frequency of each pair
 };
 
+constexpr int kPagedPromptRows = 256;   // rows of a tile of launch_paged_prompt
+
+// Two bf16 in a word: whether one is not finite, and the word with those zeroed
+__device__ inline bool bf16_pair_not_finite(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+__device__ inline uint32_t bf16_pair_finite(uint32_t w) {
+  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
+  return w;
+}
+
 // Floats of one partial result: O [rt][d], then reference, sum of the weights that O adds
 // up and sum of the unrounded weights of each row.
 __host__ __device__ inline int64_t paged_part_floats(int rt, int d) { return int64_t(rt) * (d + 3); }
@@ -78,8 +90,13 @@ hipError_t launch_paged_attn_f32(int qt, const PagedBatch& b, const PagedSplit& 
                                  const PagedTensors& t, int64_t items, int head_dim,
                                  hipStream_t stream);
 
-// Joins the parts that those launches left; tiles: at most this many per kv head.
-hipError_t launch_paged_join(int qt, const PagedBatch& b, const PagedSplit& sp,
+// Many rows per sequence (bf16): tiles of kPagedPromptRows rows.
+hipError_t launch_paged_prompt(const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
+                               int64_t items, int head_dim, hipStream_t stream);
+
+// Joins the parts that those launches left: tiles of `rows` rows, at most `tiles` of them
+// per kv head.
+hipError_t launch_paged_join(int rows, const PagedBatch& b, const PagedSplit& sp,
                              const PagedTensors& t, int64_t items, int64_t tiles, int head_dim,
                              int dtype, hipStream_t stream);
 

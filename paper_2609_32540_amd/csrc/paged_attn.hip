@@ -59,17 +59,6 @@ struct PagedCfg {
   static constexpr int kLds = kWaves * 2 * BLOCK > kJoin ? kWaves * 2 * BLOCK : kJoin;
 };
 
-__device__ inline bool not_finite(uint32_t w) {
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-}
-
-// w without its bf16 halves that are not finite
-__device__ inline uint32_t finite_halves(uint32_t w) {
-  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
-  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
-  return w;
-}
-
 template <int D, int QT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
@@ -248,13 +237,13 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 #pragma unroll
         for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
-          for (int w = 0; w < 4; ++w) bad |= not_finite(va[dt][w]);
+          for (int w = 0; w < 4; ++w) bad |= bf16_pair_not_finite(va[dt][w]);
         spread = __builtin_amdgcn_ballot_w64(bad) != 0;
         if (spread)
 #pragma unroll
           for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) va[dt][w] = finite_halves(va[dt][w]);
+            for (int w = 0; w < 4; ++w) va[dt][w] = bf16_pair_finite(va[dt][w]);
       }
     }
 
@@ -405,40 +394,92 @@ hipError_t launch(const PagedBatch& b, const PagedSplit& sp, const PagedTensors&
   return hipGetLastError();
 }
 
-// Joins the parts of the tiles that have several: workgroup (tile, kv head), thread
-// (row, 4 elements of d) after thread.
+// Joins the parts of the tiles that have several: `slices` workgroups for each tile and kv
+// head, which share the tile's outputs (rows by groups of four elements); inside a
+// workgroup groups of threads share the parts, four in flight per thread, and join through
+// LDS.  Bound by latency: a few loads deep, whatever the number of parts.
+constexpr int kJoinThreads = 256;
+
 template <class T, int D, int RT, int KB>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedBatch b, PagedSplit sp, PagedTensors t,
-                                                         int max_items) {
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, PagedSplit sp,
+                                                                  PagedTensors t, int max_items,
+                                                                  int slices) {
+  __shared__ f32x4 acc_s[kJoinThreads];
+  __shared__ float m_s[kJoinThreads], l_s[kJoinThreads], u_s[kJoinThreads];
   const int lane = threadIdx.x & 63;
-  const int head = blockIdx.x % b.kv_heads;
+  const int slice = blockIdx.x % slices, head = blockIdx.x / slices % b.kv_heads;
   PagedItem it;
-  if (!PagedScan<RT, KB>::find(b, sp, blockIdx.x / b.kv_heads, true, lane, &it)) return;
+  if (!PagedScan<RT, KB>::find(b, sp, blockIdx.x / slices / b.kv_heads, true, lane, &it)) return;
   if (it.parts <= 1 || it.item0 + it.parts > max_items) return;
   const int n_rows = min(it.seq.n_new * b.group - it.tile * RT, RT);
   const int64_t stride = paged_part_floats(RT, D);
   const float* p0 = t.part + (int64_t(it.item0) * b.kv_heads + head) * stride;
   const int64_t step = stride * b.kv_heads;   // from part to part
-  // (references are in log2 units in the bf16 kernel, in natural units in the float32 one)
+  // (references are in log2 units in the bf16 kernels, in natural units in the float32 one)
   constexpr float kUnit = sizeof(T) == 2 ? 1.0f : 1.44269504f;
-  for (int n = threadIdx.x; n < n_rows * (D / 4); n += 256) {
-    const int r = n / (D / 4), c = n % (D / 4);
-    float m = -FLT_MAX;
-    for (int p = 0; p < it.parts; ++p) m = fmaxf(m, p0[p * step + RT * D + r]);
-    float l = 0.0f, u = 0.0f;
+
+  const int outs = n_rows * (D / 4);                      // of the tile
+  const int first = int(int64_t(slice) * outs / slices), end = int(int64_t(slice + 1) * outs / slices);
+  for (int base = first; base < end; base += kJoinThreads) {
+    const int n = min(end - base, kJoinThreads);          // outputs of this round
+    const int groups = kJoinThreads / n;                  // that share the parts
+    const int g = threadIdx.x / n, i = base + threadIdx.x % n;
+    const int r = i / (D / 4), c = i % (D / 4);
+    float m = -FLT_MAX, l = 0.0f, u = 0.0f;
     f32x4 acc = {};
-    for (int p = 0; p < it.parts; ++p) {
-      const float* pp = p0 + p * step;
-      const float a = __builtin_amdgcn_exp2f((pp[RT * D + r] - m) * kUnit);
-      l += a * pp[RT * D + RT + r];
-      u += a * pp[RT * D + 2 * RT + r];
-      acc += a * *reinterpret_cast<const f32x4*>(pp + r * D + 4 * c);
+    if (g < groups)
+      for (int p = g; p < it.parts; p += 4 * groups) {
+        float pm[4], pl[4], pu[4];
+        f32x4 pa[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float* pp = p0 + min(p + k * groups, it.parts - 1) * step;
+          pm[k] = pp[RT * D + r];
+          pl[k] = pp[RT * D + RT + r];
+          pu[k] = pp[RT * D + 2 * RT + r];
+          pa[k] = *reinterpret_cast<const f32x4*>(pp + r * D + 4 * c);
+        }
+        float m_new = m;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m_new = fmaxf(m_new, p + k * groups < it.parts ? pm[k] : m_new);
+        const float a = __builtin_amdgcn_exp2f((m - m_new) * kUnit);
+        l *= a;
+        u *= a;
+        acc *= a;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (p + k * groups >= it.parts) break;
+          const float w = __builtin_amdgcn_exp2f((pm[k] - m_new) * kUnit);
+          l += w * pl[k];
+          u += w * pu[k];
+          acc += w * pa[k];
+        }
+        m = m_new;
+      }
+    m_s[threadIdx.x] = m;
+    l_s[threadIdx.x] = l;
+    u_s[threadIdx.x] = u;
+    acc_s[threadIdx.x] = acc;
+    __syncthreads();
+    if (g == 0) {
+      float m_all = m;
+      for (int k = 1; k < groups; ++k) m_all = fmaxf(m_all, m_s[threadIdx.x + k * n]);
+      l = u = 0.0f;
+      acc = f32x4{};
+      for (int k = 0; k < groups; ++k) {
+        const int x = threadIdx.x + k * n;
+        const float w = __builtin_amdgcn_exp2f((m_s[x] - m_all) * kUnit);
+        l += w * l_s[x];
+        u += w * u_s[x];
+        acc += w * acc_s[x];
+      }
+      const int row = it.tile * RT + r, tau = row / b.group;
+      const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
+                         (row - tau * b.group);
+      paged_store<T, 4>(static_cast<T*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc), l);
+      if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m_all * kUnit, u);
     }
-    const int row = it.tile * RT + r, tau = row / b.group;
-    const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
-                       (row - tau * b.group);
-    paged_store<T, 4>(static_cast<T*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc), l);
-    if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m * kUnit, u);
+    __syncthreads();
   }
 }
 
@@ -451,22 +492,30 @@ hipError_t launch_paged_attn_bf16(int qt, const PagedBatch& b, const PagedSplit&
   return qt == 2 ? launch<128, 2>(b, sp, t, items, stream) : launch<128, 1>(b, sp, t, items, stream);
 }
 
-hipError_t launch_paged_join(int qt, const PagedBatch& b, const PagedSplit& sp,
+hipError_t launch_paged_join(int rows, const PagedBatch& b, const PagedSplit& sp,
                              const PagedTensors& t, int64_t items, int64_t tiles, int head_dim,
                              int dtype, hipStream_t stream) {
-  const dim3 grid(unsigned(tiles * b.kv_heads));
+  // about two workgroups per CU, of at least 32 outputs of four elements each
+  const int64_t groups = tiles * b.kv_heads;
+  const int64_t most = int64_t(rows) * head_dim / (4 * 32);
+  int64_t slices = (2 * device_cus() + groups - 1) / groups;
+  slices = slices < most ? slices : most;
+  const dim3 grid(unsigned(groups * slices));
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, b, sp, t, int(items));
+    hipLaunchKernelGGL(kernel, grid, dim3(kJoinThreads), 0, stream, b, sp, t, int(items), int(slices));
     return hipGetLastError();
   };
   if (dtype == FF_DT_BF16) {
+    if (rows == kPagedPromptRows)
+      return head_dim == 64 ? go(paged_join_kernel<__bf16, 64, kPagedPromptRows, 64>)
+                            : go(paged_join_kernel<__bf16, 128, kPagedPromptRows, 64>);
     if (head_dim == 64)
-      return qt == 2 ? go(paged_join_kernel<__bf16, 64, 32, 32>) : go(paged_join_kernel<__bf16, 64, 16, 32>);
-    return qt == 2 ? go(paged_join_kernel<__bf16, 128, 32, 32>) : go(paged_join_kernel<__bf16, 128, 16, 32>);
+      return rows == 32 ? go(paged_join_kernel<__bf16, 64, 32, 32>) : go(paged_join_kernel<__bf16, 64, 16, 32>);
+    return rows == 32 ? go(paged_join_kernel<__bf16, 128, 32, 32>) : go(paged_join_kernel<__bf16, 128, 16, 32>);
   }
   if (head_dim == 64)
-    return qt == 2 ? go(paged_join_kernel<float, 64, 32, 16>) : go(paged_join_kernel<float, 64, 16, 16>);
-  return qt == 2 ? go(paged_join_kernel<float, 128, 32, 16>) : go(paged_join_kernel<float, 128, 16, 16>);
+    return rows == 32 ? go(paged_join_kernel<float, 64, 32, 16>) : go(paged_join_kernel<float, 64, 16, 16>);
+  return rows == 32 ? go(paged_join_kernel<float, 128, 32, 16>) : go(paged_join_kernel<float, 128, 16, 16>);
 }
 
 }  // namespace ff

@@ -82,19 +82,24 @@ __device__ inline PagedBlocks<KB> paged_blocks(const PagedBatch& b, const PagedR
 // parts; an item is (sequence, tile, part), and every kv head runs all of them.  Lengths
 // are known on the device only, so every wave finds its item by itself: it reads the
 // batch's q_start and kv_len (one element per lane) and sums in lane order, the same in
-// every wave.  Parts are of `per` blocks or a little less, `per` being what gives the
-// whole batch about `target` items (at least min_per): a ragged batch is divided by its
-// total, not by its longest sequence.  Sequences of min_rows < rows <= max_rows take part.
+// every wave.  Parts are of `per` blocks or a little less: `per` makes the whole batch, N
+// tiles, max(target, spread * N) items or a little fewer, and is at least min_per.  So a
+// ragged batch is divided by its total, not by its longest sequence, and a batch of no
+// more tiles than that (spread 0 or 1) is not divided.  Sequences of min_rows < rows <=
+// max_rows take part.
 struct PagedSplit {
-  int32_t target;     // items per kv head beyond one per tile; 0: no parts
+  int32_t target;     // 0: no parts
+  int32_t spread;
   int32_t min_per;    // blocks
   int32_t min_rows, max_rows;
 };
 
-// Most items per kv head of any batch: total / per of them, one for each tile's last part,
-// and one for the rounding of the float32 total.
-inline int64_t paged_max_items(int64_t n_tokens, int n_seqs, int group, int rt, int target) {
-  return (n_tokens * group + rt - 1) / rt + n_seqs + target + (target > 0 ? 1 : 0);
+// Most items per kv head of a batch of at most `tiles` tiles (one more for the rounding of
+// the float32 total).
+inline int64_t paged_max_items(int64_t tiles, const PagedSplit& sp) {
+  if (sp.target == 0) return tiles;
+  const int64_t most = sp.spread * tiles > sp.target ? sp.spread * tiles : sp.target;
+  return (most > tiles ? most : tiles) + 1;
 }
 
 // A value that every lane holds alike, in a scalar register
@@ -131,15 +136,21 @@ struct PagedScan {
   }
 
   __device__ static int blocks_per_part(const PagedBatch& b, const PagedSplit& sp, int lane) {
-    float total = 0.0f;
+    float total = 0.0f, n = 0.0f;
     for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
       int tiles, blocks;
       measure(b, sp, s0 + lane, &tiles, &blocks);
       total += float(tiles) * float(blocks);
+      n += float(tiles);
     }
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
-    return max(sp.min_per, int(fminf(total / float(sp.target), 1e9f)) + 1);
+    for (int d = 1; d < 64; d <<= 1) {
+      total += __shfl_xor(total, d);
+      n += __shfl_xor(n, d);
+    }
+    const float more = fmaxf(float(sp.target), float(sp.spread) * n) - n;   // items beyond one per tile
+    if (more < 1.0f) return 1 << 30;
+    return max(sp.min_per, int(fminf(total / more, 1e9f)) + 1);
   }
 
   // The item `index`; false when the batch has fewer.  by_tile: index counts tiles, not

@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <climits>
 #include <cstdio>
 #include <cstdlib>
@@ -14,6 +15,7 @@
 
 static int launches = 0;
 static size_t workspace_used = 0;
+static void* const device = reinterpret_cast<void*>(uintptr_t(0x7f0000000000));
 
 namespace ff {
 
@@ -25,14 +27,18 @@ static hipError_t batch_ok(const PagedBatch& b) {
   return ok ? hipSuccess : hipErrorInvalidValue;
 }
 
-static hipError_t attention_ok(int qt, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
+// items: at least as many as the launch's sequences can have tiles, or the target
+static hipError_t attention_ok(int rows, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
                                int64_t items, int head_dim) {
-  const int64_t tiles = (int64_t(b.n_tokens) * b.group + 16 * qt - 1) / (16 * qt);
+  const int64_t all = int64_t(b.n_tokens) * b.group;
+  int64_t tiles = all / rows;                                    // one sequence has them all
+  if (sp.max_rows < INT32_MAX)                                   // or every sequence its most
+    tiles = std::min(all / sp.max_rows, int64_t(b.n_seqs)) * ((sp.max_rows + rows - 1) / rows);
+  if (items < tiles || items < sp.target) return hipErrorInvalidValue;
   if (sp.target > 0) {
-    if (!t.part || items < tiles + b.n_seqs + sp.target) return hipErrorInvalidValue;
-    workspace_used = size_t(items) * b.kv_heads * paged_part_floats(16 * qt, head_dim) * 4;
-  } else if (items < tiles) {
-    return hipErrorInvalidValue;
+    if (!t.part || reinterpret_cast<uintptr_t>(t.part) % 16 != 0) return hipErrorInvalidValue;
+    const char* end = reinterpret_cast<const char*>(t.part) + size_t(items) * b.kv_heads * paged_part_floats(rows, head_dim) * 4;
+    workspace_used = std::max(workspace_used, size_t(end - static_cast<const char*>(device)));
   }
   return batch_ok(b);
 }
@@ -44,11 +50,15 @@ hipError_t launch_paged_append(const PagedBatch& b, const PagedAppend& a, int he
 }
 hipError_t launch_paged_attn_bf16(int qt, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
                                   int64_t items, int head_dim, hipStream_t) {
-  return attention_ok(qt, b, sp, t, items, head_dim);
+  return attention_ok(16 * qt, b, sp, t, items, head_dim);
 }
 hipError_t launch_paged_attn_f32(int qt, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
                                  int64_t items, int head_dim, hipStream_t) {
-  return attention_ok(qt, b, sp, t, items, head_dim);
+  return attention_ok(16 * qt, b, sp, t, items, head_dim);
+}
+hipError_t launch_paged_prompt(const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t, int64_t items,
+                               int head_dim, hipStream_t) {
+  return attention_ok(kPagedPromptRows, b, sp, t, items, head_dim);
 }
 hipError_t launch_paged_join(int, const PagedBatch& b, const PagedSplit& sp, const PagedTensors&, int64_t,
                              int64_t, int, int, hipStream_t) {
@@ -66,7 +76,7 @@ hipError_t launch_paged_join(int, const PagedBatch& b, const PagedSplit& sp, con
   } while (0)
 
 int main() {
-  void* dev = reinterpret_cast<void*>(uintptr_t(0x7f0000000000));
+  void* dev = device;
   const int32_t* ints = static_cast<const int32_t*>(dev);
   ff_paged_rope rope = {0, 0, 0, 0, 10000.0};
   int calls = 0;

@@ -142,6 +142,34 @@ def test_prompts(dtype, d, group, hk, block):
     c.check_attention(block=block, rows=rows)
 
 
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)])
+@pytest.mark.parametrize("kw", [dict(window=0), dict(window=1), dict(window=50, anchors=3), dict(window=300, anchors=130),
+                                dict(window=50, anchors=3, block=True), dict(window=700, block=True), dict(window=0, block=True)])
+def test_prompts_with_windows(dtype, d, kw):
+    news, lens = [300, 70, 513], [900, 500, 513]
+    rows = sorted(set(list(range(0, 883, 29)) + [0, 1, 255, 256, 299, 300, 369, 370, 371, 625, 626, 882]))
+    Case(news, lens, dtype=dtype, d=d, hk=1, group=2).check_attention(rows=rows, **kw)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)])
+@pytest.mark.parametrize("news,lens", [([300], [6000]), ([90, 1000], [5000, 3100])])
+def test_prompts_split_over_the_length(dtype, d, news, lens):
+    """Few tiles over long caches: their keys in parts."""
+    rows = [0, 1, 31, 32, 63, 64, 85, 86, 89, sum(news) // 2, sum(news) - 1]
+    for block in (False, True):
+        Case(news, lens, dtype=dtype, d=d, hk=1, group=3, page=64).check_attention(rows=rows, block=block, min_new=40)
+
+
+def test_prompts_past_64_tiles():
+    """More key tiles than a wave holds pages of, in one part (many heads), with holes."""
+    c = Case([280], [70 * 64 + 5], hk=40, group=1, d=64)
+    for col in (0, 3, 100, 255, 256, 257, 270):
+        c.b.table[0, col] = -1
+    rows = [0, 100, 255, 256, 279]
+    c.check_attention(rows=rows, heads=[0, 17, 39])
+    c.check_attention(rows=rows, heads=[0, 39], block=True)
+
+
 @pytest.mark.parametrize("hints", [dict(min_new=0, max_new=1), dict(min_new=64, max_new=64), dict(min_new=500, max_new=0)])
 def test_hints_do_not_change_what_is_computed(hints):
     """min_new and max_new that do not hold."""
@@ -221,12 +249,13 @@ def test_a_token_that_is_not_finite_reaches_only_the_rows_that_see_it(dtype, val
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_scores_far_apart(dtype):
     """Keys whose scores rise along the cache (the reference moves) and a row of one loud key."""
-    c = Case([1, 4, 90], [900, 500, 200], dtype=dtype, hk=1, group=2)
-    for s in range(3):
+    c = Case([1, 4, 90, 300], [900, 500, 200, 800], dtype=dtype, hk=1, group=2)
+    for s in range(4):
         for j in range(c.b.kv_len[s]):
             p, sl = c.b.place(s, j)
             c.k_pages[p, :, sl] *= 1.0 + j / 20.0
-    c.check_attention(rows=[0, 1, 4, 5, 30, 94])
+    c.check_attention(rows=[0, 1, 4, 5, 30, 94, 95, 200, 394], lse=False)
+    c.check_attention(rows=[0, 94, 394], block=True)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
