@@ -106,6 +106,8 @@ struct Launch {
   ff::PagedSplit split;
   int64_t tiles, items;  // at most this many per kv head
   size_t part_bytes;     // of its partial results
+  int waves;             // few rows, bf16: waves of a workgroup
+  bool once;             // and whether every sequence is one tile
 };
 struct Plan {
   Launch few, many;      // sequences of few rows, and of many
@@ -115,8 +117,9 @@ struct Plan {
 // 256-row tiles.
 constexpr int kManyRows = 64;
 
-void set_items(const ff_paged_desc& d, Launch* l, int64_t blocks) {
-  if (blocks <= l->split.min_per) l->split.target = 0;
+// blocks: of the longest sequence; none is cut that has no more than `whole` of them
+void set_items(const ff_paged_desc& d, Launch* l, int64_t blocks, int64_t whole) {
+  if (blocks <= whole) l->split.target = 0;
   l->items = ff::paged_max_items(l->tiles, l->split);
   l->part_bytes = l->split.target > 0 ? size_t(l->items) * d.num_kv_heads *
                                             ff::paged_part_floats(l->rows, d.head_dim) * 4 : 0;
@@ -136,24 +139,28 @@ Plan make_plan(const ff_paged_desc& d) {
     l.rows = most <= 16 ? 16 : 32;
     l.split.min_rows = 0;
     l.split.max_rows = many ? kManyRows : INT32_MAX;
-    l.tiles = (rows + l.rows - 1) / l.rows + d.n_seqs;
+    l.tiles = ff::paged_max_tiles(rows, d.n_seqs, l.rows);
     if (many) l.tiles = std::min(l.tiles, int64_t(d.n_seqs) * ((kManyRows + l.rows - 1) / l.rows));
     const int block = bf16 ? 32 : 16;
     l.split.min_per = 256 / block;
     l.split.target = (2 * cus + d.num_kv_heads - 1) / d.num_kv_heads;
-    l.split.spread = l.tiles * d.num_kv_heads <= 16 * cus ? 2 : 0;
-    set_items(d, &l, (keys + block - 1) / block);
+    l.split.spread = l.tiles * d.num_kv_heads <= 16 * cus ? (bf16 ? 4 : 2) : 0;
+    set_items(d, &l, (keys + block - 1) / block, 1024 / block);
+    // Short caches in more workgroups than two per CU: two waves each (no more of their
+    // blocks than two waves' copies cover are left for four), twice as many sequences at once.
+    l.waves = keys <= 512 && l.tiles * d.num_kv_heads > 2 * cus ? 2 : 4;
+    l.once = most <= l.rows;
   }
   if (many) {
     Launch& l = p.many;
     l.rows = ff::kPagedPromptRows;
     l.split.min_rows = few ? kManyRows : 0;
     l.split.max_rows = INT32_MAX;
-    l.tiles = (rows + l.rows - 1) / l.rows + (few ? std::min(int64_t(d.n_seqs), rows / kManyRows) : d.n_seqs);
+    l.tiles = ff::paged_max_tiles(rows, few ? std::min(int64_t(d.n_seqs), rows / kManyRows) : d.n_seqs, l.rows);
     l.split.min_per = 8;
     l.split.target = std::max(cus / d.num_kv_heads, 1);
-    l.split.spread = 0;
-    set_items(d, &l, (keys + 63) / 64);
+    l.split.spread = l.tiles * d.num_kv_heads <= 4 * cus ? 2 : 0;
+    set_items(d, &l, (keys + 63) / 64, l.split.min_per);
   }
   return p;
 }
@@ -164,7 +171,7 @@ hipError_t run(const Launch& l, const ff_paged_desc& d, const ff::PagedBatch& b,
   if (l.rows == ff::kPagedPromptRows)
     e = ff::launch_paged_prompt(b, l.split, t, l.items, d.head_dim, stream);
   else if (d.dtype == FF_DT_BF16)
-    e = ff::launch_paged_attn_bf16(l.rows / 16, b, l.split, t, l.items, d.head_dim, stream);
+    e = ff::launch_paged_attn_bf16(l.rows / 16, l.waves, l.once, b, l.split, t, l.items, d.head_dim, stream);
   else
     e = ff::launch_paged_attn_f32(l.rows / 16, b, l.split, t, l.items, d.head_dim, stream);
   if (e == hipSuccess && l.split.target > 0)
@@ -219,7 +226,18 @@ ff_status ff_paged_append(const ff_paged_desc* desc, const ff_paged_rope* rope, 
   a.v_stride = v_stride;
   a.n_t = r.rope_pairs_t;
   a.n_th = r.rope_pairs_t + r.rope_pairs_h;
-  ff::rope_frequencies(r.rope_pairs_t, r.rope_pairs_h, r.rope_pairs_w, r.rope_theta, a.omega);
+  // (64 powers take longer than the rest of the call: kept for the next call of this rotation)
+  struct Memo {
+    ff_paged_rope rope;
+    double omega[64];
+  };
+  static thread_local Memo memo = {};
+  if (memo.rope.rope_pairs_t != r.rope_pairs_t || memo.rope.rope_pairs_h != r.rope_pairs_h ||
+      memo.rope.rope_pairs_w != r.rope_pairs_w || memo.rope.rope_theta != r.rope_theta) {
+    ff::rope_frequencies(r.rope_pairs_t, r.rope_pairs_h, r.rope_pairs_w, r.rope_theta, memo.omega);
+    memo.rope = r;
+  }
+  std::memcpy(a.omega, memo.omega, sizeof(a.omega));
   return hip_status(ff::launch_paged_append(make_batch(d), a, d.head_dim, d.dtype,
                                             static_cast<hipStream_t>(stream)),
                     "paged_append launch");

@@ -39,6 +39,26 @@ struct PagedAppend {
   double omega[64];         // frequency of each pair
 };
 
+// lds_copy_blocks (attn_tile.h) past the caches (NT): for keys that no other workgroup reads
+template <int N, bool NT>
+__device__ inline void paged_copy(uint32_t dst, const char* base, const uint32_t (&off)[N]) {
+  static_assert(N == 2 || N == 4, "1 KB copies of 16 rows");
+  if constexpr (!NT)
+    lds_copy_blocks<N>(dst, base, off);
+  else if constexpr (N == 2)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, %3 nt\n\t"
+                 "global_load_lds_dwordx4 %2, %3 offset:1024 nt"
+                 :: "s"(dst), "v"(off[0]), "v"(off[1]), "s"(base) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+                 "global_load_lds_dwordx4 %1, %5 nt\n\t"
+                 "global_load_lds_dwordx4 %2, %5 offset:1024 nt\n\t"
+                 "global_load_lds_dwordx4 %3, %5 offset:2048 nt\n\t"
+                 "global_load_lds_dwordx4 %4, %5 offset:3072 nt"
+                 :: "s"(dst), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base) : "memory");
+}
+
 constexpr int kPagedPromptRows = 256;   // rows of a tile of launch_paged_prompt
 
 // Two bf16 in a word: whether one is not finite, and the word with those zeroed
@@ -82,9 +102,10 @@ hipError_t launch_paged_append(const PagedBatch& b, const PagedAppend& a, int he
                                hipStream_t stream);
 
 // Few rows per sequence: tiles of 16 qt rows, keys split as sp says; items: the launch's
-// items per kv head (paged_max_items).
-hipError_t launch_paged_attn_bf16(int qt, const PagedBatch& b, const PagedSplit& sp,
-                                  const PagedTensors& t, int64_t items, int head_dim,
+// items per kv head (paged_max_items); waves: 2 or 4 per workgroup; once: no key is read by
+// two tiles.
+hipError_t launch_paged_attn_bf16(int qt, int waves, bool once, const PagedBatch& b,
+                                  const PagedSplit& sp, const PagedTensors& t, int64_t items, int head_dim,
                                   hipStream_t stream);
 hipError_t launch_paged_attn_f32(int qt, const PagedBatch& b, const PagedSplit& sp,
                                  const PagedTensors& t, int64_t items, int head_dim,

@@ -35,18 +35,18 @@
 #include <float.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "ff_paged_internal.h"
 
 namespace ff {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
 constexpr int kBK = 32;            // keys per block
 constexpr float kRaise = 56.0f;    // log2 units a score may exceed the reference by: sums of
                                    // 2^56 times the keys stay far inside float32
 
-template <int D, int QT>
+template <int D, int QT, int kWaves>
 struct PagedCfg {
   static constexpr int KS = D / 32;            // 32-wide d slices of S^T
   static constexpr int DT = D / 16;            // 16-row d tiles of O^T
@@ -59,10 +59,11 @@ struct PagedCfg {
   static constexpr int kLds = kWaves * 2 * BLOCK > kJoin ? kWaves * 2 * BLOCK : kJoin;
 };
 
-template <int D, int QT>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+template <int D, int QT, int kWaves, bool NT>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
-  using C = PagedCfg<D, QT>;
+  using C = PagedCfg<D, QT, kWaves>;
+  constexpr int kThreads = 64 * kWaves;
   __shared__ __attribute__((aligned(1024))) char lds[C::kLds];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, l16 = lane & 15, grp = lane >> 4;
@@ -154,10 +155,10 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     const int j = blocks.key0(tb);
     const uint32_t dst = uint32_t(size_t(LDS_PTR(char, kbuf)));
     const int64_t a = uniform(half_offset(page0, j) - kSpan), c = uniform(half_offset(page1, j + 16) - kSpan);
-    lds_copy_blocks<C::N>(dst, kp + a, koff);
-    lds_copy_blocks<C::N>(dst + C::HALF, kp + c, koff);
-    lds_copy_blocks<C::N>(dst + C::BLOCK, vp + a, voff);
-    lds_copy_blocks<C::N>(dst + C::BLOCK + C::HALF, vp + c, voff);
+    paged_copy<C::N, NT>(dst, kp + a, koff);
+    paged_copy<C::N, NT>(dst + C::HALF, kp + c, koff);
+    paged_copy<C::N, NT>(dst + C::BLOCK, vp + a, voff);
+    paged_copy<C::N, NT>(dst + C::BLOCK + C::HALF, vp + c, voff);
   };
 
   int tb = t0 + wave, i = 0;       // this wave's i-th block
@@ -386,11 +387,14 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   }
 }
 
-template <int D, int QT>
-hipError_t launch(const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t, int64_t items,
-                  hipStream_t stream) {
-  hipLaunchKernelGGL((paged_attn_kernel<D, QT>), dim3(unsigned(items * b.kv_heads)), dim3(kThreads),
-                     0, stream, b, sp, t);
+template <int D, int QT, int W>
+hipError_t launch(bool once, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
+                  int64_t items, hipStream_t stream) {
+  const dim3 grid(unsigned(items * b.kv_heads));
+  if (once)
+    hipLaunchKernelGGL((paged_attn_kernel<D, QT, W, true>), grid, dim3(64 * W), 0, stream, b, sp, t);
+  else
+    hipLaunchKernelGGL((paged_attn_kernel<D, QT, W, false>), grid, dim3(64 * W), 0, stream, b, sp, t);
   return hipGetLastError();
 }
 
@@ -485,11 +489,20 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
 
 }  // namespace
 
-hipError_t launch_paged_attn_bf16(int qt, const PagedBatch& b, const PagedSplit& sp,
-                                  const PagedTensors& t, int64_t items, int head_dim,
-                                  hipStream_t stream) {
-  if (head_dim == 64) return qt == 2 ? launch<64, 2>(b, sp, t, items, stream) : launch<64, 1>(b, sp, t, items, stream);
-  return qt == 2 ? launch<128, 2>(b, sp, t, items, stream) : launch<128, 1>(b, sp, t, items, stream);
+hipError_t launch_paged_attn_bf16(int qt, int waves, bool once, const PagedBatch& b,
+                                  const PagedSplit& sp, const PagedTensors& t, int64_t items,
+                                  int head_dim, hipStream_t stream) {
+  auto pick = [&](auto d, auto q) {
+    constexpr int D = decltype(d)::value, Q = decltype(q)::value;
+    return waves == 2 ? launch<D, Q, 2>(once, b, sp, t, items, stream)
+                      : launch<D, Q, 4>(once, b, sp, t, items, stream);
+  };
+  using std::integral_constant;
+  if (head_dim == 64)
+    return qt == 2 ? pick(integral_constant<int, 64>{}, integral_constant<int, 2>{})
+                   : pick(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  return qt == 2 ? pick(integral_constant<int, 128>{}, integral_constant<int, 2>{})
+                 : pick(integral_constant<int, 128>{}, integral_constant<int, 1>{});
 }
 
 hipError_t launch_paged_join(int rows, const PagedBatch& b, const PagedSplit& sp,

@@ -94,12 +94,16 @@ struct PagedSplit {
   int32_t min_rows, max_rows;
 };
 
-// Most items per kv head of a batch of at most `tiles` tiles (one more for the rounding of
-// the float32 total).
+// Most tiles of n_seqs sequences of `rows` rows in all, and most items per kv head of a
+// batch of at most `tiles` tiles.
+inline int64_t paged_max_tiles(int64_t rows, int64_t n_seqs, int rt) {
+  return (rows + (rt - 1) * n_seqs) / rt;
+}
+
 inline int64_t paged_max_items(int64_t tiles, const PagedSplit& sp) {
   if (sp.target == 0) return tiles;
   const int64_t most = sp.spread * tiles > sp.target ? sp.spread * tiles : sp.target;
-  return (most > tiles ? most : tiles) + 1;
+  return most > tiles ? most : tiles;
 }
 
 // A value that every lane holds alike, in a scalar register
@@ -143,14 +147,16 @@ struct PagedScan {
       total += float(tiles) * float(blocks);
       n += float(tiles);
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
+    for (int d = 1; d < min(b.n_seqs, 64); d <<= 1) {   // (a lane behind the sequences has 0)
       total += __shfl_xor(total, d);
       n += __shfl_xor(n, d);
     }
+    total = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(total)));
+    n = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(n)));
     const float more = fmaxf(float(sp.target), float(sp.spread) * n) - n;   // items beyond one per tile
     if (more < 1.0f) return 1 << 30;
-    return max(sp.min_per, int(fminf(total / more, 1e9f)) + 1);
+    // (the factor covers the rounding of the float32 sums: never more items than the bound)
+    return max(sp.min_per, int(fminf(1.0001f * total / more, 1e9f)) + 1);
   }
 
   // The item `index`; false when the batch has fewer.  by_tile: index counts tiles, not
@@ -165,8 +171,7 @@ struct PagedScan {
       const int parts = per > 0 ? max((blocks + per - 1) / per, 1) : 1;
       const int items = tiles * parts;
       int sum = items, tsum = tiles;     // inclusive sums over the lanes
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
+      for (int d = 1; d < min(b.n_seqs - s0, 64); d <<= 1) {
         const int a = __shfl_up(sum, d), t = __shfl_up(tsum, d);
         if (lane >= d) {
           sum += a;
@@ -193,6 +198,7 @@ struct PagedScan {
         // (sums that ran over, which only a broken q_start can cause, name no item)
         return in_seq >= 0 && out->tile < n_tiles && out->item0 >= 0;
       }
+      // (only a block of 64 sequences has another behind it)
       const int all = __builtin_amdgcn_readlane(sum, 63);
       before += by_tile ? __builtin_amdgcn_readlane(tsum, 63) : all;
       items_before += all;

@@ -7,7 +7,6 @@ loading fails loudly otherwise.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -572,57 +571,94 @@ def packed_attention_bwd_static(q, k, v, out, dout, lse, dq, dk, dv, d_anchor_k=
 
 
 # ----------------------------------------------------------------------
-def _int32_on(t: torch.Tensor, device: torch.device, name: str) -> int:
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype != torch.int32 or t.device != device:
-        raise ValueError(f"{name} must be int32 on {device} (got {t.dtype} on {t.device})")
-    return t.data_ptr()
+# A decoding step makes its calls for one token, so the checks of the paged cache's calls
+# look at each property once (get_device() for the device); what is wrong is worked out
+# only once something is.
+_PAGED_DTYPES = {torch.bfloat16: FF_DT_BF16, torch.float32: FF_DT_F32}
+
+
+def _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table) -> Exception:
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages"), (q_start, "q_start"),
+                    (kv_len, "kv_len"), (page_table, "page_table")):
+        if not isinstance(t, torch.Tensor):
+            return TypeError(f"{name} must be a torch.Tensor")
+    dev, dt = k_pages.device, k_pages.dtype
+    if dt not in _PAGED_DTYPES:
+        return ValueError("dtype must be torch.bfloat16 or torch.float32")
+    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape:
+        return ValueError("k_pages and v_pages must be [num_pages][kv heads][page tokens][d]")
+    if v_pages.dtype != dt or not k_pages.is_contiguous() or not v_pages.is_contiguous():
+        return ValueError("k_pages and v_pages must be contiguous and of one dtype")
+    for t, name in ((v_pages, "v_pages"), (q_start, "q_start"), (kv_len, "kv_len"), (page_table, "page_table")):
+        if t.device != dev:
+            return ValueError(f"{name} is on {t.device}, the pool on {dev}")
+    for t, name in ((q_start, "q_start"), (kv_len, "kv_len"), (page_table, "page_table")):
+        if t.dtype != torch.int32:
+            return ValueError(f"{name} must be int32 (got {t.dtype})")
+    n = kv_len.numel()
+    if kv_len.dim() != 1 or q_start.shape != (n + 1,) or page_table.dim() != 2 or page_table.shape[0] != n:
+        return ValueError("kv_len must be [n_seqs], q_start [n_seqs + 1], page_table [n_seqs][max_pages]")
+    return ValueError("kv_len, q_start and the rows of page_table must be contiguous")
 
 
 def _paged_desc(q_heads: int, n_tokens: int, k_pages: torch.Tensor, v_pages: torch.Tensor,
                 q_start: torch.Tensor, kv_len: torch.Tensor, page_table: torch.Tensor,
                 min_new: int, max_new: int) -> PagedDesc:
-    dev, dt = k_pages.device, k_pages.dtype
-    if dt not in (torch.bfloat16, torch.float32):
-        raise ValueError("dtype must be torch.bfloat16 or torch.float32")
-    if k_pages.dim() != 4:
-        raise ValueError("k_pages must be [num_pages][kv heads][page tokens][d]")
-    _dense(k_pages, k_pages.shape, dt, dev, "k_pages")
-    _dense(v_pages, k_pages.shape, dt, dev, "v_pages")
-    n_seqs = kv_len.shape[0] if kv_len.dim() == 1 else -1
-    if n_seqs < 0 or q_start.shape != (n_seqs + 1,) or page_table.dim() != 2 or page_table.shape[0] != n_seqs:
-        raise ValueError("kv_len must be [n_seqs], q_start [n_seqs + 1], page_table [n_seqs][max_pages]")
-    if not kv_len.is_contiguous() or not q_start.is_contiguous():
-        raise ValueError("kv_len and q_start must be contiguous")
-    max_pages = page_table.shape[1]
-    stride = page_table.stride(0) if n_seqs > 1 else max_pages
-    if max_pages > 1 and page_table.stride(1) != 1:
-        raise ValueError("the rows of page_table must be contiguous")
-    return PagedDesc(k_pages.shape[0], k_pages.shape[2], q_heads, k_pages.shape[1], k_pages.shape[3],
-                     FF_DT_BF16 if dt == torch.bfloat16 else FF_DT_F32, n_seqs, n_tokens, max_pages,
-                     min_new, max_new, 0, stride, _int32_on(q_start, dev, "q_start"),
-                     _int32_on(kv_len, dev, "kv_len"), _int32_on(page_table, dev, "page_table"))
+    try:
+        num_pages, kv_heads, page_tokens, d = shape = k_pages.shape
+        (n_seqs,), (n_starts,), (n_rows, max_pages) = kv_len.shape, q_start.shape, page_table.shape
+        dt, dev, (stride, unit) = k_pages.dtype, k_pages.get_device(), page_table.stride()
+        i32 = torch.int32
+        good = (v_pages.shape == shape and v_pages.dtype is dt and k_pages.is_contiguous()
+                and v_pages.is_contiguous() and v_pages.get_device() == dev
+                and kv_len.dtype is i32 and q_start.dtype is i32 and page_table.dtype is i32
+                and kv_len.get_device() == dev and q_start.get_device() == dev
+                and page_table.get_device() == dev and n_starts == n_seqs + 1 and n_rows == n_seqs
+                and kv_len.is_contiguous() and q_start.is_contiguous() and (unit == 1 or max_pages <= 1))
+        dtype = _PAGED_DTYPES[dt]
+    except (ValueError, TypeError, AttributeError, KeyError):
+        good = False
+    if not good:
+        raise _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table)
+    return PagedDesc(num_pages, page_tokens, q_heads, kv_heads, d, dtype, n_seqs, n_tokens, max_pages,
+                     min_new, max_new, 0, stride if n_seqs > 1 else max_pages, q_start.data_ptr(),
+                     kv_len.data_ptr(), page_table.data_ptr())
 
 
-def _rows(t: torch.Tensor, like: torch.Tensor, name: str) -> Tuple[int, int]:
-    """(pointer, elements between rows) of [n_tokens][heads][d] rows of heads, each dense."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device != like.device or t.dtype != like.dtype:
-        raise ValueError(f"{name} must be {like.dtype} on {like.device} (got {t.dtype} on {t.device})")
-    d = like.shape[3]
-    if t.dim() != 3 or t.shape[2] != d:
+def _rows(t: torch.Tensor, like: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
+    """(pointer, elements between rows, rows, heads) of [n_tokens][heads][d] rows of heads, each
+    dense."""
+    if not isinstance(t, torch.Tensor) or not isinstance(like, torch.Tensor):
+        raise TypeError(f"{name} and the pool must be torch.Tensors")
+    d = like.shape[-1]
+    if t.dim() != 3 or t.size(2) != d:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [n_tokens][heads][{d}]")
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d):
+    if t.dtype is not like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be {like.dtype} on {like.device} (got {t.dtype} on {t.device})")
+    rows, heads = t.size(0), t.size(1)
+    row, head, unit = t.stride()
+    if unit != 1 or (head != d and heads > 1):
         raise ValueError(f"the heads of a row of {name} must be contiguous")
     # (a single row may report any stride)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * d
+    return t.data_ptr(), row if rows > 1 else heads * d, rows, heads
 
 
-def _on_device(device: torch.device):
-    """The tensors' device as the current one, which a launch needs."""
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+def _like(t: torch.Tensor, q: torch.Tensor, name: str) -> int:
+    """Pointer of a dense tensor of q's shape, dtype and device."""
+    if t.shape != q.shape or t.dtype != q.dtype or t.get_device() != q.get_device() or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {q.dtype} tensor of shape {tuple(q.shape)} on {q.device}")
+    return t.data_ptr()
+
+
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _call_on(index: int, fn, *args) -> int:
+    """fn(*args) with device `index` current, which a launch needs."""
+    if _get_device() == index:
+        return fn(*args)
+    with torch.cuda.device(index):
+        return fn(*args)
 
 
 def paged_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -640,38 +676,34 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_page
     Returns the rotated q (q_out, or a new tensor whose rows of no token are undefined),
     None without q.
     """
-    if k.shape != v.shape:
-        raise ValueError("k and v must have one shape")
-    n = k.shape[0]
-    dev = k_pages.device
-    desc = _paged_desc(q.shape[1] if q is not None and q.dim() == 3 else k_pages.shape[1], n, k_pages,
-                       v_pages, q_start, kv_len, page_table, 0, 0)
-    kp, ks = _rows(k, k_pages, "k")
-    vp, vs = _rows(v, k_pages, "v")
-    if k.shape[1] != k_pages.shape[1]:
-        raise ValueError(f"k has {k.shape[1]} heads, the pool {k_pages.shape[1]}")
+    kp, ks, n, heads = _rows(k, k_pages, "k")
+    vp, vs, v_rows, v_heads = _rows(v, k_pages, "v")
+    if v_rows != n or v_heads != heads or heads != k_pages.shape[1]:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} must have one shape and the pool's "
+                         f"{k_pages.shape[1]} heads")
     qp = qop = None
     qs = 0
     if q is not None:
-        qp, qs = _rows(q, k_pages, "q")
-        if q.shape[0] != n:
-            raise ValueError(f"q has {q.shape[0]} rows, k {n}")
+        qp, qs, q_rows, heads = _rows(q, k_pages, "q")
+        if q_rows != n:
+            raise ValueError(f"q has {q_rows} rows, k {n}")
         if q_out is None:
             q_out = _empty_on(q, stream)
-        qop = _dense(q_out, q.shape, q.dtype, dev, "q_out")
+        qop = _like(q_out, q, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
     pp = None
     if positions is not None:
-        if positions.shape != (n, 3) or not positions.is_contiguous():
-            raise ValueError(f"positions must be a contiguous [{n}][3] tensor")
-        pp = _int32_on(positions, dev, "positions")
-    rp = rope_pairs if rope_pairs is not None else (0, 0, 0)
-    rope = PagedRope(rp[0], rp[1], rp[2], 0, rope_theta)
-    with _on_device(dev):
-        _check(lib().ff_paged_append(ctypes.byref(desc), ctypes.byref(rope), qp, kp, vp, qs, ks, vs, pp,
-                                     qop, k_pages.data_ptr(), v_pages.data_ptr(),
-                                     _stream_handle(dev, stream)))
+        if (positions.shape != (n, 3) or positions.dtype != torch.int32 or not positions.is_contiguous()
+                or positions.get_device() != k.get_device()):
+            raise ValueError(f"positions must be a contiguous int32 [{n}][3] tensor on {k.device}")
+        pp = positions.data_ptr()
+    desc = _paged_desc(heads, n, k_pages, v_pages, q_start, kv_len, page_table, 0, 0)
+    pairs = rope_pairs if rope_pairs is not None else (0, 0, 0)
+    rope = PagedRope(pairs[0], pairs[1], pairs[2], 0, rope_theta)
+    dev = k.device
+    _check(_call_on(dev.index, lib().ff_paged_append, ctypes.byref(desc), ctypes.byref(rope), qp, kp, vp, qs,
+                    ks, vs, pp, qop, k_pages.data_ptr(), v_pages.data_ptr(), _stream_handle(dev, stream)))
     return q_out
 
 
@@ -691,30 +723,28 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     base-2 log-sum-exp.  Rows of no sequence keep what `out` holds (a new `out`: undefined).
     workspace: a uint8 tensor of paged_attention_workspace() bytes, default a new one.
     """
-    desc = _paged_desc(q.shape[1] if q.dim() == 3 else 0, q.shape[0], k_pages, v_pages, q_start, kv_len,
-                       page_table, min_new, max_new)
-    dev = k_pages.device
-    qp, qs = _rows(q, k_pages, "q")
+    qp, qs, n, heads = _rows(q, k_pages, "q")
+    desc = _paged_desc(heads, n, k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new)
+    dev = q.device
     if out is None:
         out = _empty_on(q, stream)
-    op = _dense(out, q.shape, q.dtype, dev, "out")
-    lp = _dense(lse, q.shape[:2], torch.float32, dev, "lse") if lse is not None else None
+    op = _like(out, q, "out")
+    lp = _dense(lse, (n, heads), torch.float32, dev, "lse") if lse is not None else None
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[2])
-    with _on_device(dev):
-        wp, wn = None, 0
-        if workspace is not None:
-            if workspace.device != dev or not workspace.is_contiguous():
-                raise ValueError("workspace must be a contiguous tensor on the pool's device")
-            wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        else:
-            wn = lib().ff_paged_attention_workspace(ctypes.byref(desc))
-            if wn:
-                workspace = _bytes_on(wn, dev, stream)
-                wp = workspace.data_ptr()
-        _check(lib().ff_paged_attention(ctypes.byref(desc), qp, qs, k_pages.data_ptr(), v_pages.data_ptr(),
-                                        op, lp, scale, int(block), window, anchor_tokens, wp, wn,
-                                        _stream_handle(dev, stream)))
+    ref, L = ctypes.byref(desc), lib()
+    wp, wn = None, 0
+    if workspace is not None:
+        if workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the pool's device")
+        wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    else:
+        wn = _call_on(dev.index, L.ff_paged_attention_workspace, ref)
+        if wn:
+            workspace = _bytes_on(wn, dev, stream)
+            wp = workspace.data_ptr()
+    _check(_call_on(dev.index, L.ff_paged_attention, ref, qp, qs, k_pages.data_ptr(), v_pages.data_ptr(), op,
+                    lp, scale, 1 if block else 0, window, anchor_tokens, wp, wn, _stream_handle(dev, stream)))
     return out
 
 
@@ -722,13 +752,12 @@ def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, q_start: t
                               kv_len: torch.Tensor, page_table: torch.Tensor, *, min_new: int = 0,
                               max_new: int = 0) -> int:
     """ff_paged_attention_workspace: workspace bytes of a paged_attention call (sizes only)."""
-    desc = _paged_desc(q.shape[1], q.shape[0], k_pages, k_pages, q_start, kv_len, page_table, min_new,
-                       max_new)
-    with _on_device(k_pages.device):
-        n = lib().ff_paged_attention_workspace(ctypes.byref(desc))
-    if n == 0 and lib().ff_last_error():
+    _, _, n, heads = _rows(q, k_pages, "q")
+    desc = _paged_desc(heads, n, k_pages, k_pages, q_start, kv_len, page_table, min_new, max_new)
+    bytes_ = _call_on(q.device.index, lib().ff_paged_attention_workspace, ctypes.byref(desc))
+    if bytes_ == 0 and lib().ff_last_error():
         raise FFError(1, lib().ff_last_error().decode())
-    return n
+    return bytes_
 
 
 def anchor_partition(L: int, delta: int) -> List[int]:

@@ -48,7 +48,7 @@ hipError_t launch_paged_append(const PagedBatch& b, const PagedAppend& a, int he
     if (!(a.omega[p] > 0.0)) return hipErrorInvalidValue;
   return batch_ok(b);
 }
-hipError_t launch_paged_attn_bf16(int qt, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
+hipError_t launch_paged_attn_bf16(int qt, int, bool, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
                                   int64_t items, int head_dim, hipStream_t) {
   return attention_ok(16 * qt, b, sp, t, items, head_dim);
 }
