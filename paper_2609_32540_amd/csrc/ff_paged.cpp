@@ -159,7 +159,7 @@ Plan make_plan(const ff_paged_desc& d) {
     l.tiles = ff::paged_max_tiles(rows, few ? std::min(int64_t(d.n_seqs), rows / kManyRows) : d.n_seqs, l.rows);
     l.split.min_per = 8;
     l.split.target = std::max(cus / d.num_kv_heads, 1);
-    l.split.spread = l.tiles * d.num_kv_heads <= 4 * cus ? 2 : 0;
+    l.split.spread = 0;
     set_items(d, &l, (keys + 63) / 64, l.split.min_per);
   }
   return p;
@@ -173,7 +173,7 @@ hipError_t run(const Launch& l, const ff_paged_desc& d, const ff::PagedBatch& b,
   else if (d.dtype == FF_DT_BF16)
     e = ff::launch_paged_attn_bf16(l.rows / 16, l.waves, l.once, b, l.split, t, l.items, d.head_dim, stream);
   else
-    e = ff::launch_paged_attn_f32(l.rows / 16, b, l.split, t, l.items, d.head_dim, stream);
+    e = ff::launch_paged_attn_f32(l.rows / 16, l.once, b, l.split, t, l.items, d.head_dim, stream);
   if (e == hipSuccess && l.split.target > 0)
     e = ff::launch_paged_join(l.rows, b, l.split, t, l.items, l.tiles, d.head_dim, d.dtype, stream);
   return e;

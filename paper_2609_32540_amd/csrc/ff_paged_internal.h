@@ -107,7 +107,7 @@ hipError_t launch_paged_append(const PagedBatch& b, const PagedAppend& a, int he
 hipError_t launch_paged_attn_bf16(int qt, int waves, bool once, const PagedBatch& b,
                                   const PagedSplit& sp, const PagedTensors& t, int64_t items, int head_dim,
                                   hipStream_t stream);
-hipError_t launch_paged_attn_f32(int qt, const PagedBatch& b, const PagedSplit& sp,
+hipError_t launch_paged_attn_f32(int qt, bool once, const PagedBatch& b, const PagedSplit& sp,
                                  const PagedTensors& t, int64_t items, int head_dim,
                                  hipStream_t stream);
 

@@ -71,7 +71,7 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   const int item = blockIdx.x / b.kv_heads;
 
   PagedItem it;
-  if (!PagedScan<C::kRows, kBK>::find(b, sp, item, false, lane, &it)) return;
+  if (!PagedScan<C::kRows, kBK>(b, sp, lane).find(item, false, &it)) return;
   const int n_rows = it.seq.n_new * b.group;
   const int row0 = it.tile * C::kRows;
   const int row1 = min(row0 + C::kRows, n_rows) - 1;   // last row of the tile
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
   const int lane = threadIdx.x & 63;
   const int slice = blockIdx.x % slices, head = blockIdx.x / slices % b.kv_heads;
   PagedItem it;
-  if (!PagedScan<RT, KB>::find(b, sp, blockIdx.x / slices / b.kv_heads, true, lane, &it)) return;
+  if (!PagedScan<RT, KB>(b, sp, lane).find(blockIdx.x / slices / b.kv_heads, true, &it)) return;
   if (it.parts <= 1 || it.item0 + it.parts > max_items) return;
   const int n_rows = min(it.seq.n_new * b.group - it.tile * RT, RT);
   const int64_t stride = paged_part_floats(RT, D);

@@ -24,7 +24,7 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kBK = 16;                   // keys per block
 constexpr float kLog2e = 1.44269504f;
 
-template <int D, int QT>
+template <int D, int QT, bool NT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   constexpr int KT = D / 16;              // 16-byte vectors of a K (or Q) row per lane
@@ -40,7 +40,7 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   const int item = blockIdx.x / b.kv_heads;
 
   PagedItem it;
-  if (!PagedScan<kRows, kBK>::find(b, sp, item, false, lane, &it)) return;
+  if (!PagedScan<kRows, kBK>(b, sp, lane).find(item, false, &it)) return;
   const int n_rows = it.seq.n_new * b.group;
   const int row0 = it.tile * kRows;
   const int row1 = min(row0 + kRows, n_rows) - 1;   // last row of the tile
@@ -90,18 +90,23 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   };
   const float* kpool = static_cast<const float*>(t.k_pages);
   const float* vpool = static_cast<const float*>(t.v_pages);
+  // (past the caches where no other workgroup reads the key)
+  auto load = [](const float* p) __attribute__((always_inline)) {
+    const f32x4* v = reinterpret_cast<const f32x4*>(p);
+    return NT ? __builtin_nontemporal_load(v) : *v;
+  };
   f32x4 kreg[KT], vreg[4][VH];
   auto load_k = [&](int64_t off) __attribute__((always_inline)) {
     const float* p = kpool + off + l16 * D + 4 * grp;
 #pragma unroll
-    for (int i = 0; i < KT; ++i) kreg[i] = *reinterpret_cast<const f32x4*>(p + 16 * i);
+    for (int i = 0; i < KT; ++i) kreg[i] = load(p + 16 * i);
   };
   auto load_v = [&](int64_t off) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float* p = vpool + off + (4 * grp + j) * D + 4 * l16;
 #pragma unroll
-      for (int h = 0; h < VH; ++h) vreg[j][h] = *reinterpret_cast<const f32x4*>(p + 64 * h);
+      for (int h = 0; h < VH; ++h) vreg[j][h] = load(p + 64 * h);
     }
   };
 
@@ -290,20 +295,23 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 }
 
 template <int D, int QT>
-hipError_t launch(const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t, int64_t items,
-                  hipStream_t stream) {
-  hipLaunchKernelGGL((paged_attn_f32_kernel<D, QT>), dim3(unsigned(items * b.kv_heads)),
-                     dim3(kThreads), 0, stream, b, sp, t);
+hipError_t launch(bool once, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
+                  int64_t items, hipStream_t stream) {
+  const dim3 grid(unsigned(items * b.kv_heads));
+  if (once)
+    hipLaunchKernelGGL((paged_attn_f32_kernel<D, QT, true>), grid, dim3(kThreads), 0, stream, b, sp, t);
+  else
+    hipLaunchKernelGGL((paged_attn_f32_kernel<D, QT, false>), grid, dim3(kThreads), 0, stream, b, sp, t);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_attn_f32(int qt, const PagedBatch& b, const PagedSplit& sp,
+hipError_t launch_paged_attn_f32(int qt, bool once, const PagedBatch& b, const PagedSplit& sp,
                                  const PagedTensors& t, int64_t items, int head_dim,
                                  hipStream_t stream) {
-  if (head_dim == 64) return qt == 2 ? launch<64, 2>(b, sp, t, items, stream) : launch<64, 1>(b, sp, t, items, stream);
-  return qt == 2 ? launch<128, 2>(b, sp, t, items, stream) : launch<128, 1>(b, sp, t, items, stream);
+  if (head_dim == 64) return qt == 2 ? launch<64, 2>(once, b, sp, t, items, stream) : launch<64, 1>(once, b, sp, t, items, stream);
+  return qt == 2 ? launch<128, 2>(once, b, sp, t, items, stream) : launch<128, 1>(once, b, sp, t, items, stream);
 }
 
 }  // namespace ff

@@ -122,9 +122,21 @@ struct PagedItem {
 
 template <int RT, int KB>
 struct PagedScan {
-  // tiles and an upper bound of the blocks of any of them, 0 tiles where s takes no part
-  __device__ static void measure(const PagedBatch& b, const PagedSplit& sp, int s, int* tiles,
-                                 int* blocks) {
+  const PagedBatch& b;
+  const PagedSplit& sp;
+  const int lane;
+  int tiles0, blocks0;   // of sequence `lane`
+  int per;               // blocks of a part, 0: no parts
+
+  __device__ PagedScan(const PagedBatch& batch, const PagedSplit& split, int l)
+      : b(batch), sp(split), lane(l), per(0) {
+    measure(lane, &tiles0, &blocks0);
+    if (sp.target > 0) per = blocks_per_part();
+  }
+
+  // tiles of sequence s and an upper bound of the blocks of any of them, 0 tiles where s
+  // takes no part
+  __device__ void measure(int s, int* tiles, int* blocks) const {
     *tiles = *blocks = 0;
     if (s >= b.n_seqs) return;
     const PagedSeq q = paged_seq(b, s);
@@ -138,12 +150,21 @@ struct PagedScan {
     }
     *blocks = n;
   }
+  __device__ void of_lane(int s0, int* tiles, int* blocks) const {
+    if (s0 == 0) {
+      *tiles = tiles0;
+      *blocks = blocks0;
+    } else {
+      measure(s0 + lane, tiles, blocks);
+    }
+  }
+  __device__ int parts_of(int blocks) const { return per > 0 ? max((blocks + per - 1) / per, 1) : 1; }
 
-  __device__ static int blocks_per_part(const PagedBatch& b, const PagedSplit& sp, int lane) {
+  __device__ int blocks_per_part() const {
     float total = 0.0f, n = 0.0f;
     for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
       int tiles, blocks;
-      measure(b, sp, s0 + lane, &tiles, &blocks);
+      of_lane(s0, &tiles, &blocks);
       total += float(tiles) * float(blocks);
       n += float(tiles);
     }
@@ -159,16 +180,26 @@ struct PagedScan {
     return max(sp.min_per, int(fminf(1.0001f * total / more, 1e9f)) + 1);
   }
 
+  // Items of the batch
+  __device__ int count() const {
+    int all = 0;
+    for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
+      int tiles, blocks;
+      of_lane(s0, &tiles, &blocks);
+      all += tiles * parts_of(blocks);
+    }
+    for (int d = 1; d < min(b.n_seqs, 64); d <<= 1) all += __shfl_xor(all, d);
+    return uniform(all);
+  }
+
   // The item `index`; false when the batch has fewer.  by_tile: index counts tiles, not
   // items (item0 and parts say which items a tile has).
-  __device__ static bool find(const PagedBatch& b, const PagedSplit& sp, int index, bool by_tile,
-                              int lane, PagedItem* out) {
-    const int per = sp.target > 0 ? blocks_per_part(b, sp, lane) : 0;
+  __device__ bool find(int index, bool by_tile, PagedItem* out) const {
     int before = 0, items_before = 0;   // of the sequences before s0
     for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
       int tiles, blocks;
-      measure(b, sp, s0 + lane, &tiles, &blocks);
-      const int parts = per > 0 ? max((blocks + per - 1) / per, 1) : 1;
+      of_lane(s0, &tiles, &blocks);
+      const int parts = parts_of(blocks);
       const int items = tiles * parts;
       int sum = items, tsum = tiles;     // inclusive sums over the lanes
       for (int d = 1; d < min(b.n_seqs - s0, 64); d <<= 1) {

@@ -110,24 +110,26 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   const int l16 = lane & 15;
   const int grp = lane >> 4;
 
-  // Heads are dealt to the XCDs round robin, whole (a head's tiles share its keys in one
-  // L2; the last kv_heads % 8 heads run in order), and a head's last items come first: in
-  // a causal sequence they are the longest.
+  // Workgroup bx runs on XCD bx % 8.  Heads are dealt to the XCDs round robin, whole (a head's
+  // tiles share its keys in one L2; the last kv_heads % 8 heads run in order), and a head's
+  // last items come first: in a causal sequence they are the longest.  The grid is sized for
+  // any batch of as many rows; the workgroups it has too many come last: an XCD deals its
+  // workgroups to its engines in turn whether they have work or not (with two of 21 items
+  // per head empty, 40 heads x 128, 4680 queries over 28080 keys took 2.8 instead of 2.4 ms).
+  const PagedScan<kBlockQ, kBK> scan(b, sp, lane);
+  const int n_items = gridDim.x / b.kv_heads;
+  const int n_used = min(scan.count(), n_items);
   int head, item;
   {
-    const int n_items = gridDim.x / b.kv_heads, bx = blockIdx.x;
     const int even = b.kv_heads - b.kv_heads % kXcds;
-    if (bx < even * n_items) {
-      head = bx % kXcds + kXcds * (bx / kXcds / n_items);
-      item = bx / kXcds % n_items;
-    } else {
-      head = bx / n_items;
-      item = bx % n_items;
-    }
-    item = n_items - 1 - item;
+    const bool whole = blockIdx.x < unsigned(even * n_items);
+    const int i = whole ? blockIdx.x / kXcds : blockIdx.x - even * n_items;
+    if (i >= n_used * (whole ? even / kXcds : b.kv_heads - even)) return;
+    head = whole ? blockIdx.x % kXcds + kXcds * (i / n_used) : even + i / n_used;
+    item = n_used - 1 - i % n_used;
   }
   PagedItem it;
-  if (!PagedScan<kBlockQ, kBK>::find(b, sp, item, false, lane, &it)) return;
+  if (!scan.find(item, false, &it)) return;
   const int n_rows = it.seq.n_new * b.group;
   const int row0 = it.tile * kBlockQ;
   const int row1 = min(row0 + kBlockQ, n_rows) - 1;
@@ -177,7 +179,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   }
 
   // Pages of 64 tiles: lane l holds, of tile n0 + l, the page of this wave's 16 keys (waves
-  // 0-3, which copy) and a bit for each 16 keys that are in a hole or behind the last key.
+  // 0-3, which copy) and a bit for each 16 keys that are in a hole or behind the sequence's end.
   int tp = 0, th = 0;
   auto load_pages = [&](int n0) __attribute__((always_inline)) {
     int own = 0, bits = 0;
@@ -185,7 +187,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       const int k0 = blocks.key0(t_begin + n0 + lane);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const int p = k0 + 16 * g < tail_r.hi ? paged_page(b, it.s, k0 + 16 * g) : -1;
+        const int p = k0 + 16 * g < it.seq.keys ? paged_page(b, it.s, k0 + 16 * g) : -1;
         if (p < 0) bits |= 1 << g;
         if (g == (wave & 3)) own = max(p, 0);
       }
@@ -230,7 +232,13 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   };
   // V rows of the tile at vt (first key k0) that no row of the workgroup sees become zero, and
   // where rows see different keys elements that are not finite; wave w has rows 8 w .. 8 w + 7.
+  // The fast pass does this for tiles that hold places of no token, whose memory may hold
+  // anything; tokens that are not finite are left to show in its sums (see below).
   bool bad = false;
+  auto must_clean = [&](int k0, int bits, auto pass) __attribute__((always_inline)) {
+    if constexpr (decltype(pass)::value == kPassFast) return bits != 0 || k0 + kBK > it.seq.keys;
+    else return edge(head_r, tail_r, k0, bits);
+  };
   auto clean_v = [&](char* vt, int k0, int bits) {
 #pragma unroll
     for (int c = 0; c < 8 * C::ROWB / 1024; ++c) {
@@ -333,7 +341,19 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     }
   };
   // mask the keys of a 32-key block from key j0 that a row does not see (bits: its holes)
+  const bool only_hi = last_r.lo == 0;   // every row of the wave sees all keys before its own end
   auto mask_blk = [&](f32x4 (&s)[2][kQH], int j0, int bits) __attribute__((always_inline)) {
+    if (only_hi && bits == 0) {
+#pragma unroll
+      for (int qh = 0; qh < kQH; ++qh) {
+        const int n = hi[qh] - j0 - 4 * grp;
+#pragma unroll
+        for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[kh][qh][j] = 16 * kh + j < n ? s[kh][qh][j] : -INFINITY;
+      }
+      return;
+    }
 #pragma unroll
     for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
@@ -461,7 +481,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       *reinterpret_cast<u32x4*>(slot(4) + C::TILE + C::TILE / 2 + i) = u32x4{};
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    if (edge(head_r, tail_r, k0, bits0)) {
+    if (must_clean(k0, bits0, pass)) {
       clean_v(slot(0) + C::TILE, k0, bits0);
       __syncthreads();
     }
@@ -480,7 +500,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
         if (n + 3 < n_tiles) bits3 = issue_tile(slot(i3), n + 3);
         if (n + 1 < n_tiles) {
           const int k1 = blocks.key0(t_begin + n + 1);
-          if (edge(head_r, tail_r, k1, bits1)) clean_v(slot(i1) + C::TILE, k1, bits1);
+          if (must_clean(k1, bits1, pass)) clean_v(slot(i1) + C::TILE, k1, bits1);
         }
         bits1 = bits2;
         bits2 = bits3;
@@ -533,7 +553,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       bool mask1 = false;
       if (n + 1 < n_tiles) {
         mask1 = edge(first_r, last_r, k1, bits1);
-        if (edge(head_r, tail_r, k1, bits1)) clean_v(sn + C::TILE, k1, bits1);
+        if (must_clean(k1, bits1, pass)) clean_v(sn + C::TILE, k1, bits1);
       }
       step(ka, slot(i4) + C::TILE, 1, sn, 0, s_a, s_b, pk_b, pk_a, lb, pass);
       if (mask0) mask_blk(s_b, k0 + 32, bits0 >> 2);
@@ -568,6 +588,13 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       for (int qh = 0; qh < kQH; ++qh) {
         l_tot[qh] = lsum[qh][0];
         overflow |= !(l_tot[qh] <= kFastLimit);   // (a NaN sum counts as an overflow)
+        // a V element that is not finite has made its column of O so, for every row
+        float any = 0.0f;
+#pragma unroll
+        for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) any = fmaf(o[dt][qh][j], 0.0f, any);
+        overflow |= any != 0.0f;
       }
       // One flag per wave through LDS (the tiles are no longer read after the first barrier;
       // the last one keeps the flags until every wave has read them).
@@ -589,6 +616,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
           for (int qh = 0; qh < kQH; ++qh) o[dt][qh] = f32x4{};
 #pragma unroll
         for (int qh = 0; qh < kQH; ++qh) l_run[qh] = 0.0f;
+        bad = false;
       }
     }
     if (checked_pass) {
@@ -620,7 +648,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
         // (a tile whose keys every row sees was left whole)
         int bits = 0;
         for (int g = 0; g < 4; ++g)
-          if (k0 + 16 * g >= tail_r.hi || paged_page(b, it.s, k0 + 16 * g) < 0) bits |= 1 << g;
+          if (k0 + 16 * g >= it.seq.keys || paged_page(b, it.s, k0 + 16 * g) < 0) bits |= 1 << g;
         if (!edge(head_r, tail_r, k0, bits)) continue;
 #pragma unroll
         for (int qh = 0; qh < kQH; ++qh) {

@@ -52,7 +52,7 @@ hipError_t launch_paged_attn_bf16(int qt, int, bool, const PagedBatch& b, const 
                                   int64_t items, int head_dim, hipStream_t) {
   return attention_ok(16 * qt, b, sp, t, items, head_dim);
 }
-hipError_t launch_paged_attn_f32(int qt, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
+hipError_t launch_paged_attn_f32(int qt, bool, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
                                  int64_t items, int head_dim, hipStream_t) {
   return attention_ok(16 * qt, b, sp, t, items, head_dim);
 }
