@@ -479,8 +479,10 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     // the first step adds P = 0 times the V block of a tile -1: zeros
     for (int i = 16 * tid; i < C::TILE / 2; i += 16 * kThreads)
       *reinterpret_cast<u32x4*>(slot(4) + C::TILE + C::TILE / 2 + i) = u32x4{};
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
+    // (tiles 1 and 2 may stay in flight)
+    if (n_tiles > 2) __builtin_amdgcn_s_waitcnt(waitcnt_vm(4 * C::BLOCKS_PER_WAVE));
+    else __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (must_clean(k0, bits0, pass)) {
       clean_v(slot(0) + C::TILE, k0, bits0);
       __syncthreads();
