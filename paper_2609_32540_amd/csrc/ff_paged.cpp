@@ -103,6 +103,7 @@ ff::PagedBatch make_batch(const ff_paged_desc& d) {
 // be asked for ahead of it.
 struct Launch {
   int rows;              // of a tile: 16, 32 or kPagedPromptRows; 0: no launch
+  int used;              // of them, where the batch is as its hints say
   ff::PagedSplit split;
   int64_t tiles, items;  // at most this many per kv head
   size_t part_bytes;     // of its partial results
@@ -137,6 +138,7 @@ Plan make_plan(const ff_paged_desc& d) {
   if (few) {
     Launch& l = p.few;
     l.rows = most <= 16 ? 16 : 32;
+    l.used = int(std::min(most, int64_t(l.rows)));
     l.split.min_rows = 0;
     l.split.max_rows = many ? kManyRows : INT32_MAX;
     l.tiles = ff::paged_max_tiles(rows, d.n_seqs, l.rows);
@@ -153,12 +155,16 @@ Plan make_plan(const ff_paged_desc& d) {
   }
   if (many) {
     Launch& l = p.many;
-    l.rows = ff::kPagedPromptRows;
+    l.rows = l.used = ff::kPagedPromptRows;
     l.split.min_rows = few ? kManyRows : 0;
     l.split.max_rows = INT32_MAX;
     l.tiles = ff::paged_max_tiles(rows, few ? std::min(int64_t(d.n_seqs), rows / kManyRows) : d.n_seqs, l.rows);
     l.split.min_per = 8;
-    l.split.target = std::max(cus / d.num_kv_heads, 1);
+    // Parts for launches of fewer tiles than CUs.  From three quarters of them on there is
+    // nothing to gain (two prompts of 5000 and 4000 tokens, 32/8 heads: 361 us with the join
+    // that finds no parts, 355 without; parts that even out the lengths of a causal batch
+    // cost more in partials than they save, below).
+    l.split.target = 4 * l.tiles * d.num_kv_heads >= 3 * cus ? 0 : std::max(cus / d.num_kv_heads, 1);
     l.split.spread = 0;
     set_items(d, &l, (keys + 63) / 64, l.split.min_per);
   }
@@ -175,7 +181,7 @@ hipError_t run(const Launch& l, const ff_paged_desc& d, const ff::PagedBatch& b,
   else
     e = ff::launch_paged_attn_f32(l.rows / 16, l.once, b, l.split, t, l.items, d.head_dim, stream);
   if (e == hipSuccess && l.split.target > 0)
-    e = ff::launch_paged_join(l.rows, b, l.split, t, l.items, l.tiles, d.head_dim, d.dtype, stream);
+    e = ff::launch_paged_join(l.rows, l.used, b, l.split, t, l.items, l.tiles, d.head_dim, d.dtype, stream);
   return e;
 }
 

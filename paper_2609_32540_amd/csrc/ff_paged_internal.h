@@ -115,9 +115,9 @@ hipError_t launch_paged_attn_f32(int qt, bool once, const PagedBatch& b, const P
 hipError_t launch_paged_prompt(const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
                                int64_t items, int head_dim, hipStream_t stream);
 
-// Joins the parts that those launches left: tiles of `rows` rows, at most `tiles` of them
-// per kv head.
-hipError_t launch_paged_join(int rows, const PagedBatch& b, const PagedSplit& sp,
+// Joins the parts that those launches left: tiles of `rows` rows, about `used` of them
+// used, at most `tiles` tiles per kv head.
+hipError_t launch_paged_join(int rows, int used, const PagedBatch& b, const PagedSplit& sp,
                              const PagedTensors& t, int64_t items, int64_t tiles, int head_dim,
                              int dtype, hipStream_t stream);
 

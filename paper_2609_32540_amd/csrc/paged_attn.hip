@@ -426,7 +426,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
   const int first = int(int64_t(slice) * outs / slices), end = int(int64_t(slice + 1) * outs / slices);
   for (int base = first; base < end; base += kJoinThreads) {
     const int n = min(end - base, kJoinThreads);          // outputs of this round
-    const int groups = kJoinThreads / n;                  // that share the parts
+    const int groups = min(kJoinThreads / n, (it.parts + 3) / 4);   // that share the parts
     const int g = threadIdx.x / n, i = base + threadIdx.x % n;
     const int r = i / (D / 4), c = i % (D / 4);
     float m = -FLT_MAX, l = 0.0f, u = 0.0f;
@@ -505,13 +505,16 @@ hipError_t launch_paged_attn_bf16(int qt, int waves, bool once, const PagedBatch
                  : pick(integral_constant<int, 128>{}, integral_constant<int, 1>{});
 }
 
-hipError_t launch_paged_join(int rows, const PagedBatch& b, const PagedSplit& sp,
+hipError_t launch_paged_join(int rows, int used, const PagedBatch& b, const PagedSplit& sp,
                              const PagedTensors& t, int64_t items, int64_t tiles, int head_dim,
                              int dtype, hipStream_t stream) {
-  // about two workgroups per CU, of at least 32 outputs of four elements each
+  // a workgroup for every 16 outputs of four elements, whose parts 16 groups of threads share
+  // (one sequence of 12800 tokens, one head: 20.0 us in all with 2 outputs and as many groups
+  // as fit, 14.9 with 16, 15.5 with 32), up to two per CU (12 sequences of 25 rows, 8 heads: 32.3 us
+  // with two, 34.3 with eight, since each workgroup looks its tile up)
   const int64_t groups = tiles * b.kv_heads;
-  const int64_t most = int64_t(rows) * head_dim / (4 * 32);
-  int64_t slices = (2 * device_cus() + groups - 1) / groups;
+  int64_t slices = (int64_t(used) * head_dim / 4 + 15) / 16;
+  const int64_t most = (2 * device_cus() + groups - 1) / groups;
   slices = slices < most ? slices : most;
   const dim3 grid(unsigned(groups * slices));
   auto go = [&](auto kernel) {

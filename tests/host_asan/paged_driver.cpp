@@ -60,7 +60,7 @@ hipError_t launch_paged_prompt(const PagedBatch& b, const PagedSplit& sp, const 
                                int head_dim, hipStream_t) {
   return attention_ok(kPagedPromptRows, b, sp, t, items, head_dim);
 }
-hipError_t launch_paged_join(int, const PagedBatch& b, const PagedSplit& sp, const PagedTensors&, int64_t,
+hipError_t launch_paged_join(int, int, const PagedBatch& b, const PagedSplit& sp, const PagedTensors&, int64_t,
                              int64_t, int, int, hipStream_t) {
   return sp.target > 0 ? batch_ok(b) : hipErrorInvalidValue;
 }
