@@ -71,7 +71,7 @@ __device__ inline PagedBlocks<KB> paged_blocks(const PagedBatch& b, const PagedR
                                                const PagedRange& last) {
   PagedBlocks<KB> p;
   p.lo_block = first.lo / KB;
-  p.n_anchor = (min(b.anchor_tokens, first.lo) + KB - 1) / KB;
+  p.n_anchor = (min(min(b.anchor_tokens, first.lo), last.hi) + KB - 1) / KB;
   if (p.n_anchor >= p.lo_block) p.n_anchor = p.lo_block = 0;
   p.n = p.n_anchor + max((last.hi + KB - 1) / KB - p.lo_block, 0);
   return p;

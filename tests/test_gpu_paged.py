@@ -57,37 +57,33 @@ class Case:
         return (self.k_pages.to(DEV), self.v_pages.to(DEV), torch.tensor(self.b.q_start, **i32),
                 torch.tensor(self.b.kv_len, **i32), self.b.table.to(DEV))
 
-    def check_attention(self, q=None, got=None, lse=True, scale=None, rows=None, heads=None, **kw):
-        """Run and compare; rows of no sequence have to keep what `out` held.  Returns out."""
+    def check_attention(self, q=None, scale=None, rows=None, heads=None, **kw):
+        """Run without and with the log-sum-exp (bf16 prompts then run another pass) and compare; rows
+        of no sequence have to keep what `out` held."""
         kp, vp, qs, kl, tb = self.on_gpu()
         q = q if q is not None else self.q.to(DEV)
-        out = torch.full((self.rows, self.q.shape[1], self.q.shape[2]), 7.0, dtype=self.dtype, device=DEV)
-        lse_t = torch.full(out.shape[:2], 7.0, dtype=F32, device=DEV) if lse else None
         hints = {k: kw.pop(k) for k in ("min_new", "max_new") if k in kw}
-        anchors = kw.get("anchors", 0)
         call = {k: v for k, v in kw.items() if k != "anchors"}
-        ff.paged_attention(q, kp, vp, qs, kl, tb, out=out, lse=lse_t, scale=scale, anchor_tokens=anchors,
-                           **hints, **call)
         r = ref.attention(self.b, self.q, self.k_pages, self.v_pages, scale=scale, rows=rows, heads=heads, **kw)
-        got = ref.f64(out)
         mine = r.rows if rows is None else [x for x in r.rows if x in rows]
         others = [x for x in range(self.rows) if x not in set(r.rows)]
-        assert (got[others] == 7.0).all()
         hh = list(range(self.q.shape[1])) if heads is None else list(heads)
-        a, e, tol = (x[mine][:, hh] for x in (got, r.out, r.tol))
-        nan = np.isnan(e)
-        assert (np.isnan(a) == nan).all(), "NaN in other places than the reference"
-        off = np.abs(a - e)[~nan] - tol[~nan]
-        assert off.size == 0 or off.max() <= 0, f"out off by {off.max()} over the bound"
-        if lse:
-            gl = ref.f64(lse_t)
-            assert (gl[others] == 7.0).all()
-            a, e, tol = (x[mine][:, hh] for x in (gl, r.lse, r.lse_tol))
+
+        def near(got, exact, tol):
+            assert (got[others] == 7.0).all(), "a row of no sequence was written"
+            a, e, t = (x[mine][:, hh] for x in (got, exact, tol))
             fine = np.isfinite(e)
-            assert (a[~fine & ~np.isnan(e)] == e[~fine & ~np.isnan(e)]).all()
-            assert (np.isnan(a) == np.isnan(e)).all()
-            assert (np.abs(a[fine] - e[fine]) <= tol[fine]).all(), np.abs(a[fine] - e[fine]).max()
-        return out
+            assert np.array_equal(a[~fine], e[~fine], equal_nan=True), "not finite in other places, or another value"
+            off = np.abs(a[fine] - e[fine]) - t[fine]
+            assert off.size == 0 or off.max() <= 0, f"off by {off.max()} over the bound"
+
+        for lse in (None, torch.full(self.q.shape[:2], 7.0, dtype=F32, device=DEV)):
+            out = torch.full(self.q.shape, 7.0, dtype=self.dtype, device=DEV)
+            ff.paged_attention(q, kp, vp, qs, kl, tb, out=out, lse=lse, scale=scale,
+                               anchor_tokens=kw.get("anchors", 0), **hints, **call)
+            near(ref.f64(out), r.out, r.tol)
+            if lse is not None:
+                near(ref.f64(lse), r.lse, r.lse_tol)
 
 
 # ---- attention: one new token ------------------------------------------------------
@@ -121,6 +117,12 @@ def test_decode_many_sequences():
     lens = [rng.randint(0, 90) for _ in range(333)]
     news = [min(n, rng.randint(0, 1)) for n in lens]
     Case(news, lens, hk=1, group=2, d=64).check_attention(max_new=1)
+
+
+def test_decode_most_sequences():
+    rng = random.Random(6)
+    lens = [rng.randint(1, 40) for _ in range(1024)]
+    Case([1] * 1024, lens, hk=2, group=1, d=64).check_attention(max_new=1)
 
 
 # ---- attention: several new tokens -------------------------------------------------
@@ -205,6 +207,38 @@ def test_sequences_longer_than_the_table(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("length", [100000, 2 ** 31 - 1])
+@pytest.mark.parametrize("held", [300, 320])
+def test_lengths_far_behind_the_table(dtype, length, held):
+    """Every key of the table is before the window: only the anchors are seen, and no block is
+    worked on that the table does not hold.  (300 tokens end inside a page, whose stale rest then
+    counts as tokens: NaN.)"""
+    for news in (2, 90):
+        c = Case([news], [held], dtype=dtype, hk=1, group=1, d=64)
+        c.b.kv_len[0] = length
+        kp, vp, qs, kl, tb = c.on_gpu()
+        out = torch.full_like(c.q, 7.0, device=DEV)
+        for anchors in (2 ** 31 - 1, 20, 0):
+            ff.paged_attention(c.q.to(DEV), kp, vp, qs, kl, tb, window=5, anchor_tokens=anchors, out=out)
+            near = ref.Batch([0, news], [400 + news], c.b.table, c.page, c.n_pages)   # as far behind it
+            r = ref.attention(near, c.q, c.k_pages, c.v_pages, window=5, anchors=min(anchors, 400))
+            got, nan = ref.f64(out), np.isnan(r.out)
+            assert (np.isnan(got) == nan).all() and nan.all() == (held == 300 and anchors > 300)
+            assert (np.abs(got - r.out)[~nan] <= r.tol[~nan]).all()
+
+
+@pytest.mark.parametrize("block", [False, True])
+@pytest.mark.parametrize("news,lens", [([1], [90]), ([5], [90]), ([300], [500])])
+def test_an_infinite_value_that_rows_see(block, news, lens):
+    """V holds an infinity: the columns that see it are infinite, the others are whole."""
+    c = Case(news, lens, d=64, hk=1, group=2)
+    for j, col in ((3, 5), (40, 6)):
+        p, s = c.b.place(0, j)
+        c.v_pages[p, :, s, col] = math.inf
+    c.check_attention(block=block, rows=[x for x in (0, 1, 4, 150, 299) if x < news[0]])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("news", [[1], [9], [70]])
 def test_masked_memory_does_not_matter(dtype, value, news):
@@ -254,7 +288,7 @@ def test_scores_far_apart(dtype):
         for j in range(c.b.kv_len[s]):
             p, sl = c.b.place(s, j)
             c.k_pages[p, :, sl] *= 1.0 + j / 20.0
-    c.check_attention(rows=[0, 1, 4, 5, 30, 94, 95, 200, 394], lse=False)
+    c.check_attention(rows=[0, 1, 4, 5, 30, 94, 95, 200, 394])
     c.check_attention(rows=[0, 94, 394], block=True)
 
 
