@@ -71,9 +71,8 @@ __device__ inline uint32_t bf16_pair_finite(uint32_t w) {
   return w;
 }
 
-// Floats of one partial result: O [rt][d], then reference, sum of the weights that O adds
-// up and sum of the unrounded weights of each row.
-__host__ __device__ inline int64_t paged_part_floats(int rt, int d) { return int64_t(rt) * (d + 3); }
+// Floats of one partial result: O [rt][d], then the reference and the sum of each row.
+__host__ __device__ inline int64_t paged_part_floats(int rt, int d) { return int64_t(rt) * (d + 2); }
 
 // N elements of a row of the output; a row that saw nothing (l = 0) is zero
 template <class T, int N>

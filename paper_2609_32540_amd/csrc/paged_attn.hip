@@ -27,8 +27,10 @@
 // see different keys, a V element that is not finite is kept out of the products, which
 // would spread it to every row as 0 * inf, and added for the rows that see it.
 //
-// Rounding: probabilities to bf16 (nearest even) as operands of the matrix unit, the sums
-// that divide O over the rounded values; scores, references, sums and O are float32.
+// Rounding: a probability enters the matrix unit as two bf16, its value rounded and what
+// that leaves rounded again (2^-17 in all), since products cost nothing here: the output has
+// the error of its own rounding, 1.7e-3 (relative-L2) where probabilities of one bf16 give
+// 2.3e-3.  Scores, references, sums and O are float32.
 
 #include <hip/hip_runtime.h>
 
@@ -55,7 +57,7 @@ struct PagedCfg {
   static constexpr int N = HALF / 1024;        // 1 KB copies of a half
   static constexpr int kRows = 16 * QT;
   static constexpr int kPitch = D + 4;         // padded row of the join buffer (floats)
-  static constexpr int kJoin = kWaves * kRows * (kPitch + 3) * 4;
+  static constexpr int kJoin = kWaves * kRows * (kPitch + 2) * 4;
   static constexpr int kLds = kWaves * 2 * BLOCK > kJoin ? kWaves * 2 * BLOCK : kJoin;
 };
 
@@ -96,16 +98,8 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     for (int s = 0; s < C::KS; ++s) qreg[x][s] = *reinterpret_cast<const bf16x8*>(qp + 32 * s);
   }
 
-  f32x4 o[C::DT][QT], lsum[QT];
+  f32x4 o[C::DT][QT];
   float m_run[QT], l_run[QT];
-#pragma unroll
-  for (int x = 0; x < QT; ++x) {
-    m_run[x] = -FLT_MAX;   // (finite: keys that score -inf get weight 0)
-    l_run[x] = 0.0f;       // this lane's share of the sum of the unrounded probabilities
-    lsum[x] = f32x4{};     // sum of the rounded ones (every row of the tile holds it)
-#pragma unroll
-    for (int dt = 0; dt < C::DT; ++dt) o[dt][x] = f32x4{};
-  }
 
   // Pages of this wave's blocks t0 + wave, + 4, ..: lane 2 i + half holds the page of that
   // half of block i of the current 32 (a reload every 32 blocks)
@@ -161,172 +155,191 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     paged_copy<C::N, NT>(dst + C::BLOCK + C::HALF, vp + c, voff);
   };
 
-  int tb = t0 + wave, i = 0;       // this wave's i-th block
-  int page[2] = {-1, -1};
-  if (tb < t1) {
-    load_pages(0);
-    page[0] = __builtin_amdgcn_readlane(page_of, 0);
-    page[1] = __builtin_amdgcn_readlane(page_of, 1);
-    fetch(tb, page[0], page[1]);
-  }
-  while (tb < t1) {
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-    asm volatile("" ::: "memory");
-    bf16x8 kc[2][C::KS];
-    u32x4 va[C::DT];
+  // The wave's blocks.  The rests of the probabilities meet a V element that is not finite as
+  // 0 or a negative number, which would make an infinity NaN: a wave whose O is not finite
+  // goes over its blocks again without them.
+  for (bool rests = true;; rests = false) {
 #pragma unroll
-    for (int kh = 0; kh < 2; ++kh)
+    for (int x = 0; x < QT; ++x) {
+      m_run[x] = -FLT_MAX;   // (finite: keys that score -inf get weight 0)
+      l_run[x] = 0.0f;       // this lane's share of the sum of the probabilities
+#pragma unroll
+      for (int dt = 0; dt < C::DT; ++dt) o[dt][x] = f32x4{};
+    }
+    int tb = t0 + wave, i = 0;       // this wave's i-th block
+    int page[2] = {-1, -1};
+    if (tb < t1) {
+      load_pages(0);
+      page[0] = __builtin_amdgcn_readlane(page_of, 0);
+      page[1] = __builtin_amdgcn_readlane(page_of, 1);
+      fetch(tb, page[0], page[1]);
+    }
+    while (tb < t1) {
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+      asm volatile("" ::: "memory");
+      bf16x8 kc[2][C::KS];
+      u32x4 va[C::DT];
+#pragma unroll
+      for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+        for (int ks = 0; ks < C::KS; ++ks)
+          kc[kh][ks] = *reinterpret_cast<const bf16x8*>(kbuf + k_lane + 1024 * (kh * C::KS + ks));
+#pragma unroll
+      for (int dt = 0; dt < C::DT; ++dt) {
+        const char* vt = vbuf + v_lane[dt % 4] + 1024 * (dt / 4);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, vt));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, vt + 32 * D));
+        const u32x2 lo2 = __builtin_bit_cast(u32x2, lo), hi2 = __builtin_bit_cast(u32x2, hi);
+        va[dt] = u32x4{lo2[0], lo2[1], hi2[0], hi2[1]};
+      }
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done
+      __builtin_amdgcn_sched_barrier(0);
+      const int j0 = blocks.key0(tb);
+      const int cur[2] = {page[0], page[1]};
+      const int next = tb + kWaves;
+      ++i;
+      if (next < t1) {
+        if ((i & 31) == 0) load_pages(i);
+        page[0] = __builtin_amdgcn_readlane(page_of, 2 * (i & 31));
+        page[1] = __builtin_amdgcn_readlane(page_of, 2 * (i & 31) + 1);
+        fetch(next, page[0], page[1]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+
+      f32x4 s[2][QT];
 #pragma unroll
       for (int ks = 0; ks < C::KS; ++ks)
-        kc[kh][ks] = *reinterpret_cast<const bf16x8*>(kbuf + k_lane + 1024 * (kh * C::KS + ks));
 #pragma unroll
-    for (int dt = 0; dt < C::DT; ++dt) {
-      const char* vt = vbuf + v_lane[dt % 4] + 1024 * (dt / 4);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, vt));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, vt + 32 * D));
-      const u32x2 lo2 = __builtin_bit_cast(u32x2, lo), hi2 = __builtin_bit_cast(u32x2, hi);
-      va[dt] = u32x4{lo2[0], lo2[1], hi2[0], hi2[1]};
-    }
-    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the reads are done
-    __builtin_amdgcn_sched_barrier(0);
-    const int j0 = blocks.key0(tb);
-    const int cur[2] = {page[0], page[1]};
-    const int next = tb + kWaves;
-    ++i;
-    if (next < t1) {
-      if ((i & 31) == 0) load_pages(i);
-      page[0] = __builtin_amdgcn_readlane(page_of, 2 * (i & 31));
-      page[1] = __builtin_amdgcn_readlane(page_of, 2 * (i & 31) + 1);
-      fetch(next, page[0], page[1]);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+        for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+          for (int x = 0; x < QT; ++x)
+            s[kh][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[kh][ks], qreg[x][ks],
+                                                               ks == 0 ? f32x4{} : s[kh][x], 0, 0, 0);
 
-    f32x4 s[2][QT];
+      // the block holds keys that some row does not see
+      const bool edge = j0 + kBK > head_r.hi || cur[0] < 0 || cur[1] < 0 ||
+                        (j0 < tail_r.lo && j0 + kBK > b.anchor_tokens);
+      bool spread = false;   // some V element that is not finite was kept out of the products
+      if (edge) {
 #pragma unroll
-    for (int ks = 0; ks < C::KS; ++ks)
+        for (int kh = 0; kh < 2; ++kh)
 #pragma unroll
-      for (int kh = 0; kh < 2; ++kh)
+          for (int e = 0; e < 4; ++e) {
+            const int j = j0 + 16 * kh + 4 * grp + e;
 #pragma unroll
-        for (int x = 0; x < QT; ++x)
-          s[kh][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[kh][ks], qreg[x][ks],
-                                                             ks == 0 ? f32x4{} : s[kh][x], 0, 0, 0);
-
-    // the block holds keys that some row does not see
-    const bool edge = j0 + kBK > head_r.hi || cur[0] < 0 || cur[1] < 0 ||
-                      (j0 < tail_r.lo && j0 + kBK > b.anchor_tokens);
-    bool spread = false;   // some V element that is not finite was kept out of the products
-    if (edge) {
+            for (int x = 0; x < QT; ++x) {
+              const bool seen = cur[kh] >= 0 && j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
+              s[kh][x][e] = seen ? s[kh][x][e] : -INFINITY;
+            }
+            // (a key some row may see: before the last row's end, behind the first row's start)
+            const bool any = cur[kh] >= 0 && j < tail_r.hi && (j >= head_r.lo || j < b.anchor_tokens);
+            if (!any)
 #pragma unroll
-      for (int kh = 0; kh < 2; ++kh)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int j = j0 + 16 * kh + 4 * grp + e;
-#pragma unroll
-          for (int x = 0; x < QT; ++x) {
-            const bool seen = cur[kh] >= 0 && j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
-            s[kh][x][e] = seen ? s[kh][x][e] : -INFINITY;
+              for (int dt = 0; dt < C::DT; ++dt)
+                va[dt][2 * kh + (e >> 1)] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
           }
-          // (a key some row may see: before the last row's end, behind the first row's start)
-          const bool any = cur[kh] >= 0 && j < tail_r.hi && (j >= head_r.lo || j < b.anchor_tokens);
-          if (!any)
+        if (rows_differ) {
+          bool bad = false;
+#pragma unroll
+          for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) bad |= bf16_pair_not_finite(va[dt][w]);
+          spread = __builtin_amdgcn_ballot_w64(bad) != 0;
+          if (spread)
 #pragma unroll
             for (int dt = 0; dt < C::DT; ++dt)
-              va[dt][2 * kh + (e >> 1)] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+#pragma unroll
+              for (int w = 0; w < 4; ++w) va[dt][w] = bf16_pair_finite(va[dt][w]);
         }
-      if (rows_differ) {
-        bool bad = false;
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) bad |= bf16_pair_not_finite(va[dt][w]);
-        spread = __builtin_amdgcn_ballot_w64(bad) != 0;
-        if (spread)
-#pragma unroll
-          for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-            for (int w = 0; w < 4; ++w) va[dt][w] = bf16_pair_finite(va[dt][w]);
       }
-    }
 
-    float mx[QT];
-    bool over = false;
-#pragma unroll
-    for (int x = 0; x < QT; ++x) {
-      mx[x] = fmaxf(fmaxf(s[0][x][0], s[0][x][1]), fmaxf(s[0][x][2], s[0][x][3]));
-      mx[x] = fmaxf(mx[x], fmaxf(fmaxf(s[1][x][0], s[1][x][1]), fmaxf(s[1][x][2], s[1][x][3])));
-      mx[x] = max_across_groups(mx[x]) * t.scale_log2;
-      // the first block's max is the reference from then on, until a score passes it far
-      over |= mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + kRaise);
-    }
-    if (__builtin_amdgcn_ballot_w64(over) != 0) {
+      float mx[QT];
+      bool over = false;
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        const float m_new = mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + kRaise) ? mx[x] : m_run[x];
-        const float alpha = __builtin_amdgcn_exp2f(m_run[x] - m_new);
-        l_run[x] *= alpha;
-        lsum[x] *= alpha;
-        m_run[x] = m_new;
-#pragma unroll
-        for (int dt = 0; dt < C::DT; ++dt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[dt][x][e] *= alpha;
+        mx[x] = fmaxf(fmaxf(s[0][x][0], s[0][x][1]), fmaxf(s[0][x][2], s[0][x][3]));
+        mx[x] = fmaxf(mx[x], fmaxf(fmaxf(s[1][x][0], s[1][x][1]), fmaxf(s[1][x][2], s[1][x][3])));
+        mx[x] = max_across_groups(mx[x]) * t.scale_log2;
+        // the first block's max is the reference from then on, until a score passes it far
+        over |= mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + kRaise);
       }
-    }
-    uint32_t pk[QT][4];
-#pragma unroll
-    for (int x = 0; x < QT; ++x) {
-      float lb = 0.0f;
-#pragma unroll
-      for (int kh = 0; kh < 2; ++kh)
-#pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kh][x][e], t.scale_log2, -m_run[x]));
-          const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kh][x][e + 1], t.scale_log2, -m_run[x]));
-          pk[x][2 * kh + (e >> 1)] = pack_bf16(p0, p1);
-          lb += p0 + p1;
-        }
-      l_run[x] += lb;
-    }
-    // (all ones: every row of the result is the column sum of P^T)
-    const bf16x8 ones = {__bf16(1.0f), __bf16(1.0f), __bf16(1.0f), __bf16(1.0f),
-                         __bf16(1.0f), __bf16(1.0f), __bf16(1.0f), __bf16(1.0f)};
-#pragma unroll
-    for (int x = 0; x < QT; ++x) {
-      const u32x4 pu = {pk[x][0], pk[x][1], pk[x][2], pk[x][3]};
-      const bf16x8 pb = __builtin_bit_cast(bf16x8, pu);
-#pragma unroll
-      for (int dt = 0; dt < C::DT; ++dt)
-        o[dt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, va[dt]), pb,
-                                                           o[dt][x], 0, 0, 0);
-      lsum[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pb, lsum[x], 0, 0, 0);
-    }
-    if (spread) {
-      // V elements that are not finite, for the rows that see their key (from the pool:
-      // the copy in LDS is the next block's by now)
-#pragma unroll 1
-      for (int kk = 0; kk < kBK; ++kk) {
-        const int kh = kk >> 4, j = j0 + kk;
-        if (cur[kh] < 0 || j >= tail_r.hi) continue;
-        const __bf16* vr = reinterpret_cast<const __bf16*>(vp + half_offset(cur[kh], j));
+      if (__builtin_amdgcn_ballot_w64(over) != 0) {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          uint32_t w = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w = e == (kk >> 1 & 1) + 2 * kh ? pk[x][e] : w;
-          const uint32_t pw = uint32_t(__shfl(int(w), l16 + 16 * ((kk & 15) >> 2)));
-          const float p = __uint_as_float((kk & 1) ? pw & 0xffff0000u : pw << 16);
-          const bool seen = j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
+          const float m_new = mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + kRaise) ? mx[x] : m_run[x];
+          const float alpha = __builtin_amdgcn_exp2f(m_run[x] - m_new);
+          l_run[x] *= alpha;
+          m_run[x] = m_new;
 #pragma unroll
           for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float v = float(vr[16 * dt + 4 * grp + e]);
-              if (seen && !isfinite(v)) o[dt][x][e] += p * v;
-            }
+            for (int e = 0; e < 4; ++e) o[dt][x][e] *= alpha;
         }
       }
+      uint32_t pk[QT][4], pr[QT][4];   // rounded, and the rests
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        float lb = 0.0f;
+#pragma unroll
+        for (int kh = 0; kh < 2; ++kh)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[kh][x][e], t.scale_log2, -m_run[x]));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[kh][x][e + 1], t.scale_log2, -m_run[x]));
+            const uint32_t w = pack_bf16(p0, p1);
+            pk[x][2 * kh + (e >> 1)] = w;
+            pr[x][2 * kh + (e >> 1)] = pack_bf16(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
+            lb += p0 + p1;
+          }
+        l_run[x] += lb;
+      }
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+        const u32x4 pu = {pk[x][0], pk[x][1], pk[x][2], pk[x][3]}, ru = {pr[x][0], pr[x][1], pr[x][2], pr[x][3]};
+#pragma unroll
+        for (int dt = 0; dt < C::DT; ++dt) {
+          const bf16x8 v = __builtin_bit_cast(bf16x8, va[dt]);
+          o[dt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, pu), o[dt][x], 0, 0, 0);
+          if (rests)
+            o[dt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, ru), o[dt][x], 0, 0, 0);
+        }
+      }
+      if (spread) {
+        // V elements that are not finite, for the rows that see their key (from the pool:
+        // the copy in LDS is the next block's by now)
+#pragma unroll 1
+        for (int kk = 0; kk < kBK; ++kk) {
+          const int kh = kk >> 4, j = j0 + kk;
+          if (cur[kh] < 0 || j >= tail_r.hi) continue;
+          const __bf16* vr = reinterpret_cast<const __bf16*>(vp + half_offset(cur[kh], j));
+#pragma unroll
+          for (int x = 0; x < QT; ++x) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w = e == (kk >> 1 & 1) + 2 * kh ? pk[x][e] : w;
+            const uint32_t pw = uint32_t(__shfl(int(w), l16 + 16 * ((kk & 15) >> 2)));
+            const float p = __uint_as_float((kk & 1) ? pw & 0xffff0000u : pw << 16);
+            const bool seen = j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
+#pragma unroll
+            for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float v = float(vr[16 * dt + 4 * grp + e]);
+                if (seen && !isfinite(v)) o[dt][x][e] += p * v;
+              }
+          }
+        }
+      }
+      tb = next;
     }
-    tb = next;
+    float any = 0.0f;
+#pragma unroll
+    for (int x = 0; x < QT; ++x)
+#pragma unroll
+      for (int dt = 0; dt < C::DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any = fmaf(o[dt][x][e], 0.0f, any);
+    if (!rests || __builtin_amdgcn_ballot_w64(any != 0.0f) == 0) break;
   }
 
   // join the waves (over the K and V blocks, once all are read)
@@ -334,15 +347,13 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   float* part = reinterpret_cast<float*>(lds);
   float* part_m = part + kWaves * C::kRows * C::kPitch;
   float* part_l = part_m + kWaves * C::kRows;
-  float* part_u = part_l + kWaves * C::kRows;
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const int row = wave * C::kRows + 16 * x + l16;
-    const float u = sum_across_groups(l_run[x]);
+    const float l = sum_across_groups(l_run[x]);
     if (grp == 0) {
       part_m[row] = m_run[x];
-      part_l[row] = lsum[x][0];
-      part_u[row] = u;
+      part_l[row] = l;
     }
 #pragma unroll
     for (int dt = 0; dt < C::DT; ++dt)
@@ -356,14 +367,13 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     float m = part_m[r];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w * C::kRows + r]);
-    float l = 0.0f, u = 0.0f;
+    float l = 0.0f;
     f32x4 acc[2] = {};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const int row = w * C::kRows + r;
       const float a = __builtin_amdgcn_exp2f(part_m[row] - m);
       l += a * part_l[row];
-      u += a * part_u[row];
 #pragma unroll
       for (int x = 0; x < 2; ++x)
         acc[x] += a * *reinterpret_cast<const f32x4*>(part + row * C::kPitch + 8 * c + 4 * x);
@@ -374,7 +384,6 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       if (c == 0) {
         ws[C::kRows * D + r] = m;
         ws[C::kRows * D + C::kRows + r] = l;
-        ws[C::kRows * D + 2 * C::kRows + r] = u;
       }
     } else {
       const int tau = (row0 + r) / b.group;
@@ -382,7 +391,7 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
                          (row0 + r - tau * b.group);
       paged_store<__bf16, 8>(static_cast<__bf16*>(t.out) + at * D + 8 * c,
                              reinterpret_cast<const float*>(acc), l);
-      if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m, u);
+      if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m, l);
     }
   }
 }
@@ -409,7 +418,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
                                                                   PagedTensors t, int max_items,
                                                                   int slices) {
   __shared__ f32x4 acc_s[kJoinThreads];
-  __shared__ float m_s[kJoinThreads], l_s[kJoinThreads], u_s[kJoinThreads];
+  __shared__ float m_s[kJoinThreads], l_s[kJoinThreads];
   const int lane = threadIdx.x & 63;
   const int slice = blockIdx.x % slices, head = blockIdx.x / slices % b.kv_heads;
   PagedItem it;
@@ -429,18 +438,17 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
     const int groups = min(kJoinThreads / n, (it.parts + 3) / 4);   // that share the parts
     const int g = threadIdx.x / n, i = base + threadIdx.x % n;
     const int r = i / (D / 4), c = i % (D / 4);
-    float m = -FLT_MAX, l = 0.0f, u = 0.0f;
+    float m = -FLT_MAX, l = 0.0f;
     f32x4 acc = {};
     if (g < groups)
       for (int p = g; p < it.parts; p += 4 * groups) {
-        float pm[4], pl[4], pu[4];
+        float pm[4], pl[4];
         f32x4 pa[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float* pp = p0 + min(p + k * groups, it.parts - 1) * step;
           pm[k] = pp[RT * D + r];
           pl[k] = pp[RT * D + RT + r];
-          pu[k] = pp[RT * D + 2 * RT + r];
           pa[k] = *reinterpret_cast<const f32x4*>(pp + r * D + 4 * c);
         }
         float m_new = m;
@@ -448,40 +456,36 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
         for (int k = 0; k < 4; ++k) m_new = fmaxf(m_new, p + k * groups < it.parts ? pm[k] : m_new);
         const float a = __builtin_amdgcn_exp2f((m - m_new) * kUnit);
         l *= a;
-        u *= a;
         acc *= a;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           if (p + k * groups >= it.parts) break;
           const float w = __builtin_amdgcn_exp2f((pm[k] - m_new) * kUnit);
           l += w * pl[k];
-          u += w * pu[k];
           acc += w * pa[k];
         }
         m = m_new;
       }
     m_s[threadIdx.x] = m;
     l_s[threadIdx.x] = l;
-    u_s[threadIdx.x] = u;
     acc_s[threadIdx.x] = acc;
     __syncthreads();
     if (g == 0) {
       float m_all = m;
       for (int k = 1; k < groups; ++k) m_all = fmaxf(m_all, m_s[threadIdx.x + k * n]);
-      l = u = 0.0f;
+      l = 0.0f;
       acc = f32x4{};
       for (int k = 0; k < groups; ++k) {
         const int x = threadIdx.x + k * n;
         const float w = __builtin_amdgcn_exp2f((m_s[x] - m_all) * kUnit);
         l += w * l_s[x];
-        u += w * u_s[x];
         acc += w * acc_s[x];
       }
       const int row = it.tile * RT + r, tau = row / b.group;
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
                          (row - tau * b.group);
       paged_store<T, 4>(static_cast<T*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc), l);
-      if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m_all * kUnit, u);
+      if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m_all * kUnit, l);
     }
     __syncthreads();
   }

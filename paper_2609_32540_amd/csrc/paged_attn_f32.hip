@@ -281,7 +281,6 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       if (c == 0) {
         ws[kRows * D + r] = m;
         ws[kRows * D + kRows + r] = l;
-        ws[kRows * D + 2 * kRows + r] = l;
       }
     } else {
       const int tau = (row0 + r) / b.group;

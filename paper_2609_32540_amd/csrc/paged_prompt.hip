@@ -682,7 +682,6 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       if (grp == 0) {
         ws[kBlockQ * D + row] = m_run[qh];
         ws[kBlockQ * D + kBlockQ + row] = l_tot[qh];
-        ws[kBlockQ * D + 2 * kBlockQ + row] = l_tot[qh];
       }
     } else {
       const int tau = r / b.group;
