@@ -95,6 +95,8 @@ ff::PagedBatch make_batch(const ff_paged_desc& d) {
   b.page_shift = __builtin_ctz(unsigned(d.page_tokens));
   b.kv_heads = d.num_kv_heads;
   b.group = d.num_q_heads / d.num_kv_heads;
+  while ((1 << b.group_shift) < b.group) ++b.group_shift;
+  b.group_magic = uint32_t(((uint64_t(1) << (31 + b.group_shift)) + b.group - 1) / b.group);
   b.window = -1;
   return b;
 }

@@ -77,8 +77,8 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   const int n_rows = it.seq.n_new * b.group;
   const int row0 = it.tile * C::kRows;
   const int row1 = min(row0 + C::kRows, n_rows) - 1;   // last row of the tile
-  const PagedRange head_r = paged_range(b, it.seq, row0 / b.group);
-  const PagedRange tail_r = paged_range(b, it.seq, row1 / b.group);
+  const PagedRange head_r = paged_range(b, it.seq, paged_token(b, row0));
+  const PagedRange tail_r = paged_range(b, it.seq, paged_token(b, row1));
   const PagedBlocks<kBK> blocks = paged_blocks<kBK>(b, head_r, tail_r);
   const int t0 = uniform(int(int64_t(it.part) * blocks.n / it.parts));
   const int t1 = uniform(int(int64_t(it.part + 1) * blocks.n / it.parts));
@@ -90,7 +90,7 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const int r = min(row0 + 16 * x + l16, row1);
-    const int tau = r / b.group;
+    const int tau = paged_token(b, r);
     see[x] = paged_range(b, it.seq, tau);
     const __bf16* qp = static_cast<const __bf16*>(t.q) + int64_t(it.seq.q0 + tau) * t.q_stride +
                        int64_t(head * b.group + r - tau * b.group) * D + 8 * grp;
@@ -386,7 +386,7 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
         ws[C::kRows * D + C::kRows + r] = l;
       }
     } else {
-      const int tau = (row0 + r) / b.group;
+      const int tau = paged_token(b, row0 + r);
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
                          (row0 + r - tau * b.group);
       paged_store<__bf16, 8>(static_cast<__bf16*>(t.out) + at * D + 8 * c,
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
         l += w * l_s[x];
         acc += w * acc_s[x];
       }
-      const int row = it.tile * RT + r, tau = row / b.group;
+      const int row = it.tile * RT + r, tau = paged_token(b, row);
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
                          (row - tau * b.group);
       paged_store<T, 4>(static_cast<T*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc), l);

@@ -44,8 +44,8 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   const int n_rows = it.seq.n_new * b.group;
   const int row0 = it.tile * kRows;
   const int row1 = min(row0 + kRows, n_rows) - 1;   // last row of the tile
-  const PagedRange head_r = paged_range(b, it.seq, row0 / b.group);
-  const PagedRange tail_r = paged_range(b, it.seq, row1 / b.group);
+  const PagedRange head_r = paged_range(b, it.seq, paged_token(b, row0));
+  const PagedRange tail_r = paged_range(b, it.seq, paged_token(b, row1));
   const PagedBlocks<kBK> blocks = paged_blocks<kBK>(b, head_r, tail_r);
   const int t0 = uniform(int(int64_t(it.part) * blocks.n / it.parts));
   const int t1 = uniform(int(int64_t(it.part + 1) * blocks.n / it.parts));
@@ -56,7 +56,7 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 #pragma unroll
   for (int x = 0; x < QT; ++x) {
     const int r = min(row0 + 16 * x + l16, row1);
-    const int tau = r / b.group;
+    const int tau = paged_token(b, r);
     see[x] = paged_range(b, it.seq, tau);
     const float* qp = static_cast<const float*>(t.q) + int64_t(it.seq.q0 + tau) * t.q_stride +
                       int64_t(head * b.group + r - tau * b.group) * D + 4 * grp;
@@ -283,7 +283,7 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
         ws[kRows * D + kRows + r] = l;
       }
     } else {
-      const int tau = (row0 + r) / b.group;
+      const int tau = paged_token(b, row0 + r);
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
                          (row0 + r - tau * b.group);
       paged_store<float, 4>(static_cast<float*>(t.out) + at * D + 4 * c,

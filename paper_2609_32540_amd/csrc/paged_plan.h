@@ -24,10 +24,18 @@ struct PagedBatch {
   int32_t page_shift;          // log2 of the tokens per page
   int32_t kv_heads;
   int32_t group;               // query heads per kv head
+  uint32_t group_magic;        // ceil(2^(31 + group_shift) / group)
+  int32_t group_shift;         // ceil(log2(group))
   int32_t window;              // -1: no bound
   int32_t anchor_tokens;
   int32_t block;               // 1: the new tokens see each other
 };
+
+// Token of row r (r / group; exact for 0 <= r < 2^31: the magic number is off by less than
+// group <= 2^group_shift in 2^(31 + group_shift)), a fifth of a division's instructions
+__device__ inline int paged_token(const PagedBatch& b, int r) {
+  return int(__umulhi(2u * uint32_t(r), b.group_magic) >> b.group_shift);
+}
 
 // Sequence s: its new tokens are rows q0 .. q0 + n_new - 1; token tau has index
 // first + tau (negative: there is no such token); keys 0 .. keys - 1 are in its pages.
@@ -125,21 +133,23 @@ struct PagedScan {
   const PagedBatch& b;
   const PagedSplit& sp;
   const int lane;
-  int tiles0, blocks0;   // of sequence `lane`
+  PagedSeq seq0;         // sequence `lane`
+  int tiles0, blocks0;
   int per;               // blocks of a part, 0: no parts
 
   __device__ PagedScan(const PagedBatch& batch, const PagedSplit& split, int l)
       : b(batch), sp(split), lane(l), per(0) {
-    measure(lane, &tiles0, &blocks0);
+    of_sequence(lane, &seq0, &tiles0, &blocks0);
     if (sp.target > 0) per = blocks_per_part();
   }
 
-  // tiles of sequence s and an upper bound of the blocks of any of them, 0 tiles where s
+  // sequence s, its tiles and an upper bound of the blocks of any of them, 0 tiles where s
   // takes no part
-  __device__ void measure(int s, int* tiles, int* blocks) const {
+  __device__ void of_sequence(int s, PagedSeq* seq, int* tiles, int* blocks) const {
     *tiles = *blocks = 0;
+    *seq = PagedSeq{0, 0, 0, 0};
     if (s >= b.n_seqs) return;
-    const PagedSeq q = paged_seq(b, s);
+    const PagedSeq q = *seq = paged_seq(b, s);
     const int64_t rows = int64_t(q.n_new) * b.group;
     if (rows <= sp.min_rows || rows > sp.max_rows) return;
     *tiles = int((rows + RT - 1) / RT);
@@ -150,12 +160,13 @@ struct PagedScan {
     }
     *blocks = n;
   }
-  __device__ void of_lane(int s0, int* tiles, int* blocks) const {
+  __device__ void of_lane(int s0, PagedSeq* seq, int* tiles, int* blocks) const {
     if (s0 == 0) {
+      *seq = seq0;
       *tiles = tiles0;
       *blocks = blocks0;
     } else {
-      measure(s0 + lane, tiles, blocks);
+      of_sequence(s0 + lane, seq, tiles, blocks);
     }
   }
   __device__ int parts_of(int blocks) const { return per > 0 ? max((blocks + per - 1) / per, 1) : 1; }
@@ -163,8 +174,9 @@ struct PagedScan {
   __device__ int blocks_per_part() const {
     float total = 0.0f, n = 0.0f;
     for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
+      PagedSeq seq;
       int tiles, blocks;
-      of_lane(s0, &tiles, &blocks);
+      of_lane(s0, &seq, &tiles, &blocks);
       total += float(tiles) * float(blocks);
       n += float(tiles);
     }
@@ -184,8 +196,9 @@ struct PagedScan {
   __device__ int count() const {
     int all = 0;
     for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
+      PagedSeq seq;
       int tiles, blocks;
-      of_lane(s0, &tiles, &blocks);
+      of_lane(s0, &seq, &tiles, &blocks);
       all += tiles * parts_of(blocks);
     }
     for (int d = 1; d < min(b.n_seqs, 64); d <<= 1) all += __shfl_xor(all, d);
@@ -197,8 +210,9 @@ struct PagedScan {
   __device__ bool find(int index, bool by_tile, PagedItem* out) const {
     int before = 0, items_before = 0;   // of the sequences before s0
     for (int s0 = 0; s0 < b.n_seqs; s0 += 64) {
+      PagedSeq seq;
       int tiles, blocks;
-      of_lane(s0, &tiles, &blocks);
+      of_lane(s0, &seq, &tiles, &blocks);
       const int parts = parts_of(blocks);
       const int items = tiles * parts;
       int sum = items, tsum = tiles;     // inclusive sums over the lanes
@@ -220,8 +234,8 @@ struct PagedScan {
         // (every lane holds the same: kept where the addresses made of it stay scalar)
         const int tile = by_tile ? in_seq : in_seq / n_parts;
         out->s = uniform(s0 + l);
-        const PagedSeq q = paged_seq(b, out->s);
-        out->seq = {uniform(q.q0), uniform(q.n_new), uniform(q.first), uniform(q.keys)};
+        out->seq = {__builtin_amdgcn_readlane(seq.q0, l), __builtin_amdgcn_readlane(seq.n_new, l),
+                    __builtin_amdgcn_readlane(seq.first, l), __builtin_amdgcn_readlane(seq.keys, l)};
         out->parts = uniform(n_parts);
         out->tile = uniform(tile);
         out->part = uniform(by_tile ? 0 : in_seq - tile * n_parts);

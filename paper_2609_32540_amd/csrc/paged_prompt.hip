@@ -133,8 +133,8 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   const int n_rows = it.seq.n_new * b.group;
   const int row0 = it.tile * kBlockQ;
   const int row1 = min(row0 + kBlockQ, n_rows) - 1;
-  const PagedRange head_r = paged_range(b, it.seq, row0 / b.group);    // first and last row
-  const PagedRange tail_r = paged_range(b, it.seq, row1 / b.group);
+  const PagedRange head_r = paged_range(b, it.seq, paged_token(b, row0));    // first and last row
+  const PagedRange tail_r = paged_range(b, it.seq, paged_token(b, row1));
   const bool rows_differ = head_r.hi != tail_r.hi || head_r.lo != tail_r.lo;
   const PagedBlocks<kBK> blocks = paged_blocks<kBK>(b, head_r, tail_r);
   const int t_begin = uniform(int(int64_t(it.part) * blocks.n / it.parts));
@@ -149,7 +149,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 #pragma unroll
   for (int qh = 0; qh < kQH; ++qh) {
     const int r = min(q0 + 16 * qh + l16, row1);
-    const int tau = r / b.group;
+    const int tau = paged_token(b, r);
     const PagedRange see = paged_range(b, it.seq, tau);
     hi[qh] = see.hi;
     lo[qh] = see.lo;
@@ -159,8 +159,8 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     for (int s = 0; s < C::KS; ++s) qreg[qh][s] = *reinterpret_cast<const bf16x8*>(qp + 32 * s);
   }
   // this wave's first and last row
-  const PagedRange first_r = paged_range(b, it.seq, min(q0, row1) / b.group);
-  const PagedRange last_r = paged_range(b, it.seq, min(q0 + kWaveQ - 1, row1) / b.group);
+  const PagedRange first_r = paged_range(b, it.seq, paged_token(b, min(q0, row1)));
+  const PagedRange last_r = paged_range(b, it.seq, paged_token(b, min(q0 + kWaveQ - 1, row1)));
 
   // O^T tile (d tile dt, row half qh): lane (l16, grp) holds row q0 + 16 qh + l16 at
   // d = 16 dt + 4 grp + j, j = 0 .. 3
@@ -684,7 +684,7 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
         ws[kBlockQ * D + kBlockQ + row] = l_tot[qh];
       }
     } else {
-      const int tau = r / b.group;
+      const int tau = paged_token(b, r);
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group + (r - tau * b.group);
 #pragma unroll
       for (int dt = 0; dt < C::DT; ++dt)
