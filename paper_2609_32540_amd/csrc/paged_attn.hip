@@ -466,28 +466,31 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
         }
         m = m_new;
       }
-    m_s[threadIdx.x] = m;
-    l_s[threadIdx.x] = l;
-    acc_s[threadIdx.x] = acc;
-    __syncthreads();
-    if (g == 0) {
-      float m_all = m;
-      for (int k = 1; k < groups; ++k) m_all = fmaxf(m_all, m_s[threadIdx.x + k * n]);
-      l = 0.0f;
-      acc = f32x4{};
-      for (int k = 0; k < groups; ++k) {
-        const int x = threadIdx.x + k * n;
-        const float w = __builtin_amdgcn_exp2f((m_s[x] - m_all) * kUnit);
-        l += w * l_s[x];
-        acc += w * acc_s[x];
+    if (groups > 1) {   // (uniform)
+      m_s[threadIdx.x] = m;
+      l_s[threadIdx.x] = l;
+      acc_s[threadIdx.x] = acc;
+      __syncthreads();
+      if (g == 0) {
+        for (int k = 1; k < groups; ++k) m = fmaxf(m, m_s[threadIdx.x + k * n]);
+        l = 0.0f;
+        acc = f32x4{};
+        for (int k = 0; k < groups; ++k) {
+          const int x = threadIdx.x + k * n;
+          const float w = __builtin_amdgcn_exp2f((m_s[x] - m) * kUnit);
+          l += w * l_s[x];
+          acc += w * acc_s[x];
+        }
       }
+      __syncthreads();
+    }
+    if (g == 0) {
       const int row = it.tile * RT + r, tau = paged_token(b, row);
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
                          (row - tau * b.group);
       paged_store<T, 4>(static_cast<T*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc), l);
-      if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m_all * kUnit, l);
+      if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m * kUnit, l);
     }
-    __syncthreads();
   }
 }
 
@@ -514,11 +517,11 @@ hipError_t launch_paged_join(int rows, int used, const PagedBatch& b, const Page
                              int dtype, hipStream_t stream) {
   // a workgroup for every 16 outputs of four elements, whose parts 16 groups of threads share
   // (one sequence of 12800 tokens, one head: 20.0 us in all with 2 outputs and as many groups
-  // as fit, 14.9 with 16, 15.5 with 32), up to two per CU (12 sequences of 25 rows, 8 heads: 32.3 us
+  // as fit, 14.9 with 16, 15.5 with 32), up to two per CU, four for the 256-row tiles (12 sequences of 25 rows, 8 heads: 32.3 us
   // with two, 34.3 with eight, since each workgroup looks its tile up)
   const int64_t groups = tiles * b.kv_heads;
   int64_t slices = (int64_t(used) * head_dim / 4 + 15) / 16;
-  const int64_t most = (2 * device_cus() + groups - 1) / groups;
+  const int64_t most = ((rows > 32 ? 4 : 2) * device_cus() + groups - 1) / groups;
   slices = slices < most ? slices : most;
   const dim3 grid(unsigned(groups * slices));
   auto go = [&](auto kernel) {
