@@ -116,9 +116,30 @@ struct Plan {
   Launch few, many;      // sequences of few rows, and of many
 };
 
-// Rows (new tokens x query heads per kv head) from which a sequence goes to the kernel of
-// 256-row tiles.
-constexpr int kManyRows = 64;
+// Rows (new tokens x query heads per kv head) above which a sequence goes to the kernel of
+// 256-row tiles where a batch runs both: up to here one tile of the other reads each key
+// once.
+constexpr int kManyRows = 32;
+
+// Whether a bf16 batch runs on the kernel of few rows alone, by estimated times (us): that
+// kernel reads the keys once from HBM and again, mostly from L2, for every further tile of
+// 32 rows; the other takes equal time for its key blocks, one tile's at the least, and a
+// fixed part for prologue, partials and join, and for the first one's launch where it is
+// needed as well.  The constants are fits to 1 to 64
+// sequences x 48 to 256 rows x 300 to 30000 keys and to prompts of 20 to 2000 tokens, either
+// kernel forced: 2 sequences x 588 tokens over 2350 keys, 2 heads 24 against 34; 5 prompts of
+// up to 300 tokens, 5 heads 11 against 31; 8 x 48 rows x 4000 keys, 12 heads 80 against 55; 1170
+// tokens over 7000 keys, 12 heads 132 against 69.  Keys are counted by the table's columns.
+bool few_rows_alone(const ff_paged_desc& d, int64_t rows, bool both, double keys, int cus) {
+  const double seqs = std::min(d.n_seqs, d.n_tokens);
+  const double key_bytes = 4.0 * d.head_dim * d.num_kv_heads;
+  const double more = std::max(double(rows) / 32 - 0.5 * seqs, 0.0);   // tiles beyond one each
+  const double few = 8.0 + seqs * keys * key_bytes / 5.5e6 + more * keys * key_bytes / 9e6;
+  const double step = d.head_dim == 128 ? 1.7 : 1.0;   // a 64-key block of a 256-row tile
+  const double units = double(ff::paged_max_tiles(rows, int64_t(seqs), ff::kPagedPromptRows)) * d.num_kv_heads;
+  const double many = 20.0 + (both ? 10.0 : 0.0) + step * std::max(units * keys / 64 / cus, std::min(keys / 64, 8.0));
+  return few <= many;
+}
 
 // blocks: of the longest sequence; none is cut that has no more than `whole` of them
 void set_items(const ff_paged_desc& d, Launch* l, int64_t blocks, int64_t whole) {
@@ -136,7 +157,9 @@ Plan make_plan(const ff_paged_desc& d) {
   const int64_t most = (d.max_new > 0 ? std::min(d.max_new, d.n_tokens) : d.n_tokens) * int64_t(group);
   const int64_t keys = int64_t(d.max_pages) * d.page_tokens;
   const bool bf16 = d.dtype == FF_DT_BF16;
-  const bool many = bf16 && most > kManyRows, few = !many || int64_t(d.min_new) * group <= kManyRows;
+  const bool some_few = int64_t(d.min_new) * group <= kManyRows;
+  const bool many = bf16 && most > kManyRows && !few_rows_alone(d, rows, some_few, double(keys), cus);
+  const bool few = !many || some_few;
   if (few) {
     Launch& l = p.few;
     l.rows = most <= 16 ? 16 : 32;
