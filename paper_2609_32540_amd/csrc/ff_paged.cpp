@@ -196,6 +196,12 @@ Plan make_plan(const ff_paged_desc& d) {
   return p;
 }
 
+// The forms that the calling thread's last attention call took (exported as
+// ff_internal_last_paged, not part of the C ABI), so that a test can tell that it reached
+// the one it is about: rows of a tile of few rows (0: not launched) and whether its keys
+// could be cut, the same of many rows.
+thread_local int32_t last_paged[4] = {};
+
 hipError_t run(const Launch& l, const ff_paged_desc& d, const ff::PagedBatch& b,
                const ff::PagedTensors& t, hipStream_t stream) {
   hipError_t e;
@@ -213,6 +219,8 @@ hipError_t run(const Launch& l, const ff_paged_desc& d, const ff::PagedBatch& b,
 }  // namespace
 
 extern "C" {
+
+int32_t ff_internal_last_paged(int32_t field) { return field >= 0 && field < 4 ? last_paged[field] : -1; }
 
 ff_status ff_paged_append(const ff_paged_desc* desc, const ff_paged_rope* rope, const void* q,
                           const void* k, const void* v, int64_t q_stride, int64_t k_stride,
@@ -326,6 +334,8 @@ ff_status ff_paged_attention(const ff_paged_desc* desc, const void* q, int64_t q
   t.scale = softmax_scale;
   t.scale_log2 = float(double(softmax_scale) * 1.4426950408889634);
   const hipStream_t hs = static_cast<hipStream_t>(stream);
+  const int32_t forms[4] = {p.few.rows, p.few.split.target > 0, p.many.rows, p.many.split.target > 0};
+  std::copy(forms, forms + 4, last_paged);
   hipError_t e = hipSuccess;
   if (p.few.rows > 0) e = run(p.few, d, b, t, hs);
   t.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.few.part_bytes);

@@ -20,6 +20,12 @@ BF16, F32 = torch.bfloat16, torch.float32
 DEV = torch.device("cuda", 0)
 
 
+def forms():
+    """The forms of this thread's last call: rows of the tiles of few rows (0: not launched), whether
+    their keys could be cut, the same of many rows."""
+    return tuple(ff.lib().ff_internal_last_paged(i) for i in range(4))
+
+
 class Case:
     """A pool, a batch and tensors.  news, lens: new tokens and lengths of the sequences; unused
     pool memory holds `stale` (NaN by default)."""
@@ -57,7 +63,7 @@ class Case:
         return (self.k_pages.to(DEV), self.v_pages.to(DEV), torch.tensor(self.b.q_start, **i32),
                 torch.tensor(self.b.kv_len, **i32), self.b.table.to(DEV))
 
-    def check_attention(self, q=None, scale=None, rows=None, heads=None, **kw):
+    def check_attention(self, q=None, scale=None, rows=None, heads=None, form=None, **kw):
         """Run without and with the log-sum-exp (bf16 prompts then run another pass) and compare; rows
         of no sequence have to keep what `out` held."""
         kp, vp, qs, kl, tb = self.on_gpu()
@@ -81,6 +87,8 @@ class Case:
             out = torch.full(self.q.shape, 7.0, dtype=self.dtype, device=DEV)
             ff.paged_attention(q, kp, vp, qs, kl, tb, out=out, lse=lse, scale=scale,
                                anchor_tokens=kw.get("anchors", 0), **hints, **call)
+            if form is not None and self.dtype == BF16:
+                assert forms() == form
             near(ref.f64(out), r.out, r.tol)
             if lse is not None:
                 near(ref.f64(lse), r.lse, r.lse_tol)
@@ -134,42 +142,112 @@ def test_several_new_tokens(dtype, d, block, window, anchors):
     Case(news, lens, dtype=dtype, d=d, hk=2, group=3).check_attention(block=block, window=window, anchors=anchors)
 
 
+# Small launches of many rows run on the kernel of few rows (tiles of 16 or 32), so what is said
+# of the 256-row one is tested at many heads, a few of them checked.
+FEW, MANY, BOTH = (32, 0, 0, 0), (0, 0, 256, 0), (32, 1, 256, 0)
+
+
 @pytest.mark.parametrize("dtype,d,group,hk", [(BF16, 128, 4, 2), (BF16, 64, 1, 3), (BF16, 128, 1, 1), (F32, 128, 2, 1)])
 @pytest.mark.parametrize("block", [False, True])
-def test_prompts(dtype, d, group, hk, block):
+def test_small_prompts(dtype, d, group, hk, block):
     """Prompts of several tiles, ragged, the first one starting at key 0; sampled rows."""
     news, lens = [700, 129, 1, 64], [700, 400, 350, 77]
     c = Case(news, lens, dtype=dtype, d=d, group=group, hk=hk)
     rows = sorted(set(list(range(0, 700, 37)) + [0, 1, 63, 64, 255, 256, 699, 700, 701, 828, 829, 830, 893]))
-    c.check_attention(block=block, rows=rows)
+    c.check_attention(block=block, rows=rows, form=FEW)
+
+
+@pytest.mark.parametrize("d,group,hk", [(128, 4, 16), (128, 1, 40), (64, 3, 30), (64, 1, 64)])
+@pytest.mark.parametrize("block", [False, True])
+def test_prompts(d, group, hk, block):
+    """The same on the 256-row kernel, beside a sequence of one new token."""
+    news, lens = [900, 300, 1, 70, 0], [900, 1100, 950, 77, 30]
+    c = Case(news, lens, d=d, group=group, hk=hk)
+    rows = [0, 1, 31, 32, 63, 64, 65, 85, 255, 256, 257, 640, 899, 900, 901, 1199, 1200, 1201, 1202, 1270]
+    c.check_attention(block=block, rows=rows, heads=[0, hk * group - 1], form=BOTH)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("kw", [dict(window=0), dict(window=1), dict(window=50, anchors=3), dict(window=300, anchors=130),
+                                dict(window=2000, anchors=5), dict(window=50, anchors=3, block=True),
+                                dict(window=700, block=True), dict(window=0, block=True)])
+def test_prompts_with_windows(d, kw):
+    news, lens = [600, 70, 1013], [1200, 500, 1013]
+    rows = [0, 1, 31, 32, 127, 128, 255, 256, 599, 600, 601, 669, 670, 671, 700, 800, 925, 926, 1682]
+    Case(news, lens, d=d, hk=64, group=1).check_attention(rows=rows, heads=[0, 63], form=MANY, min_new=70, **kw)
 
 
 @pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)])
-@pytest.mark.parametrize("kw", [dict(window=0), dict(window=1), dict(window=50, anchors=3), dict(window=300, anchors=130),
-                                dict(window=50, anchors=3, block=True), dict(window=700, block=True), dict(window=0, block=True)])
-def test_prompts_with_windows(dtype, d, kw):
+@pytest.mark.parametrize("kw", [dict(window=0), dict(window=50, anchors=3), dict(window=300, anchors=130),
+                                dict(window=50, anchors=3, block=True), dict(window=700, block=True)])
+def test_small_prompts_with_windows(dtype, d, kw):
     news, lens = [300, 70, 513], [900, 500, 513]
     rows = sorted(set(list(range(0, 883, 29)) + [0, 1, 255, 256, 299, 300, 369, 370, 371, 625, 626, 882]))
-    Case(news, lens, dtype=dtype, d=d, hk=1, group=2).check_attention(rows=rows, **kw)
+    Case(news, lens, dtype=dtype, d=d, hk=1, group=2).check_attention(rows=rows, form=FEW, **kw)
 
 
-@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)])
-@pytest.mark.parametrize("news,lens", [([300], [6000]), ([90, 1000], [5000, 3100])])
-def test_prompts_split_over_the_length(dtype, d, news, lens):
+@pytest.mark.parametrize("d,hk,news,lens", [(128, 4, [1000], [16000]), (64, 6, [300, 700], [18000, 17000]), (128, 8, [90, 600], [5000, 9100])])
+def test_prompts_split_over_the_length(d, hk, news, lens):
     """Few tiles over long caches: their keys in parts."""
     rows = [0, 1, 31, 32, 63, 64, 85, 86, 89, sum(news) // 2, sum(news) - 1]
     for block in (False, True):
-        Case(news, lens, dtype=dtype, d=d, hk=1, group=3, page=64).check_attention(rows=rows, block=block, min_new=40)
+        c = Case(news, lens, d=d, hk=hk, group=1, page=64)
+        c.check_attention(rows=rows, heads=[0, hk - 1], block=block, min_new=90, form=(0, 0, 256, 1))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)])
+def test_small_prompts_split_over_the_length(dtype, d):
+    for block in (False, True):
+        c = Case([90, 200], [5000, 3100], dtype=dtype, d=d, hk=1, group=3, page=64)
+        c.check_attention(rows=[0, 31, 32, 89, 90, 200, 289], block=block, form=(32, 1, 0, 0))
 
 
 def test_prompts_past_64_tiles():
-    """More key tiles than a wave holds pages of, in one part (many heads), with holes."""
-    c = Case([280], [70 * 64 + 5], hk=40, group=1, d=64)
+    """More key tiles than a wave holds pages of, in one part, with holes."""
+    c = Case([1280], [70 * 64 + 5], hk=64, group=1, d=64)
     for col in (0, 3, 100, 255, 256, 257, 270):
         c.b.table[0, col] = -1
-    rows = [0, 100, 255, 256, 279]
-    c.check_attention(rows=rows, heads=[0, 17, 39])
-    c.check_attention(rows=rows, heads=[0, 39], block=True)
+    rows = [0, 100, 255, 256, 279, 1279]
+    c.check_attention(rows=rows, heads=[0, 63], min_new=1280, form=MANY)
+    c.check_attention(rows=rows, heads=[0, 63], block=True, min_new=1280, form=MANY)
+
+
+@pytest.mark.parametrize("bad", [-1, 2 ** 31 - 1])
+def test_prompts_with_holes(bad):
+    """At the start, inside, everywhere; stale memory behind the end."""
+    c = Case([600, 500, 300], [900, 1000, 300], hk=64, group=1, d=64)
+    c.b.table[0, 0] = c.b.table[0, 5] = bad
+    c.b.table[1, 30:40] = bad
+    c.b.table[2, :] = bad
+    rows = [0, 1, 300, 599, 600, 700, 1099, 1100, 1399]
+    for kw in (dict(), dict(block=True, window=160, anchors=20)):
+        c.check_attention(rows=rows, heads=[0, 63], min_new=300, form=MANY, **kw)
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf])
+def test_prompt_tokens_that_are_not_finite(value):
+    """Causal: V (then K) of one token is not finite, the rows before it are whole."""
+    news, length, hk = 700, 1000, 64
+    for which in ("v", "k"):
+        c = Case([news], [length], d=64, hk=hk, group=1)
+        j = length - news + 333
+        p, s = c.b.place(0, j)
+        if which == "v":
+            c.v_pages[p, :, s, 3] = value
+        else:
+            c.k_pages[p, :, s] = value
+        rows = [0, 255, 256, 300, 332] + ([333, 340, 699] if which == "v" else [])
+        c.check_attention(rows=rows, heads=[0, 40], min_new=news, form=MANY)
+
+
+def test_prompt_scores_far_apart():
+    """The reference of the first block is left far behind: the checked pass, in parts and whole."""
+    for news, length, hk, form in ((1000, 1100, 64, MANY), (256, 24000, 4, (0, 0, 256, 1))):
+        c = Case([news], [length], d=128, hk=hk, group=1, page=64)
+        for col in range(c.b.table.shape[1]):
+            c.k_pages[int(c.b.table[0, col])] *= 1.0 + 3.0 * col * 64 / length * 20
+        for block in (False, True):
+            c.check_attention(rows=[0, 40, 255, news - 1], heads=[0, hk - 1], block=block, min_new=news, form=form)
 
 
 @pytest.mark.parametrize("hints", [dict(min_new=0, max_new=1), dict(min_new=64, max_new=64), dict(min_new=500, max_new=0)])
