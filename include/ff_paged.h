@@ -126,9 +126,10 @@ size_t ff_paged_attention_workspace(const ff_paged_desc* desc);
  * [num_q_heads][head_dim].  lse (optional, device, [n_tokens][num_q_heads] float) receives
  * the base-2 log-sum-exp of each row's scaled scores, -inf for a row that sees none.
  * Arithmetic as ff_chunk_attention: bf16 products on the matrix cores with float32
- * accumulation, softmax in float32, probabilities and output rounded to bf16 (nearest
- * even); f32 float32 throughout.  How the keys are split, and with it the last bits of a
- * row, depends on the whole batch; the same call gives the same bits.
+ * accumulation, softmax in float32, probabilities (in sequences of few rows: and the rests of
+ * that rounding) and output rounded to bf16 (nearest even); f32 float32 throughout.  How the
+ * keys are split, and with it the last bits of a row, depends on the whole batch; the same
+ * call gives the same bits.  One to four kernel launches, by the sizes in `desc`.
  * workspace (device, 16-byte aligned, ff_paged_attention_workspace() bytes) is the call's
  * until its work is done: calls that may overlap, graphs among them, need one each.  out
  * and lse must not overlap anything else. */

@@ -31,6 +31,14 @@
 // that leaves rounded again (2^-17 in all), since products cost nothing here: the output has
 // the error of its own rounding, 1.7e-3 (relative-L2) where probabilities of one bf16 give
 // 2.3e-3.  Scores, references, sums and O are float32.
+//
+// Measured (32/8 heads x 128, cold, joins included).  64 sequences of 150 to 12000 tokens:
+// 257 us = 5.9 TB/s, within 1% of the copies alone (the kernel without its operand reads and
+// products); read through the caches 284 us, so a key that no other tile reads is read past
+// them.  One sequence of 32773 tokens: 33 us, of which the join is 6 (1.3 its launch, 0.7 the
+// lookup); with twice the parts 42.  Two waves per workgroup, four workgroups per CU: 274
+// and 35, but 55 instead of 82 for 250 sequences of up to 308 tokens, 12 kv heads (and so
+// they are chosen there).
 
 #include <hip/hip_runtime.h>
 

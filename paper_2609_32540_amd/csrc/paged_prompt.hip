@@ -19,6 +19,14 @@
 //   passes   the fast pass needs a first block that every row sees a key of, which a causal
 //            window does not give: those, and calls that want the log-sum-exp (the sum of the
 //            unrounded probabilities), run the checked pass at once.
+//   rounding probabilities as one bf16, the sums over the rounded values, as there: a second
+//            product for their rests would cost half of the products again.
+//
+// Measured (32/8 heads x 128).  Prompts of 5003 and 3966 tokens, causal: 354 us = 1040 TFLOP/s
+// of the visible pairs; 16384 tokens as one block 1290 TFLOP/s.  40 heads, 4680 queries over
+// 28080 keys 2.33 ms (attn_bf16.hip over a ring 2.31).  A 64-key step takes 1.7 us, a tile about
+// 14 us beside its steps: workgroup launch, lookup and Q 7.5, the pages and the first copies
+// 6.5, which nothing covers, as all of a CU's LDS is one workgroup's.
 
 #include <hip/hip_runtime.h>
 
