@@ -680,8 +680,8 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 #pragma unroll
   for (int qh = 0; qh < kQH; ++qh) {
     const int r = q0 + 16 * qh + l16;
-    if (r > row1) continue;
     if (it.parts > 1) {
+      if (r > row1) continue;
       float* ws = t.part + (int64_t(item) * b.kv_heads + head) * paged_part_floats(kBlockQ, D);
       const int row = r - row0;
 #pragma unroll
@@ -692,13 +692,34 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
         ws[kBlockQ * D + kBlockQ + row] = l_tot[qh];
       }
     } else {
-      const int tau = paged_token(b, r);
-      const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group + (r - tau * b.group);
+      // a row that saw nothing (l = 0) is zero
+      const float inv = 1.0f / l_tot[qh];
+      const bool some = l_tot[qh] != 0.0f;
+      uint32_t w[C::DT][2];
 #pragma unroll
       for (int dt = 0; dt < C::DT; ++dt)
-        paged_store<__bf16, 4>(static_cast<__bf16*>(t.out) + at * D + 16 * dt + 4 * grp,
-                               reinterpret_cast<const float*>(&o[dt][qh]), l_tot[qh]);
-      if (t.lse != nullptr && grp == 0) t.lse[at] = paged_lse(m_run[qh], l_tot[qh]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          w[dt][h] = some ? pack_bf16(o[dt][qh][2 * h] * inv, o[dt][qh][2 * h + 1] * inv) : 0u;
+      const int tau = paged_token(b, min(r, row1));
+      const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
+                         (min(r, row1) - tau * b.group);
+      __bf16* op = static_cast<__bf16*>(t.out) + at * D + 8 * grp;
+      // two d tiles, 8 bytes of each per lane, become 16 bytes in a row: lane group g takes
+      // d = 32 k + 8 g .. +7
+#pragma unroll
+      for (int k = 0; k < C::DT / 2; ++k) {
+        uint32_t lo[2], hi2[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          auto x = __builtin_amdgcn_permlane32_swap(w[2 * k][h], w[2 * k + 1][h], false, false);
+          x = __builtin_amdgcn_permlane16_swap(x[0], x[1], false, false);
+          lo[h] = x[0];
+          hi2[h] = x[1];
+        }
+        if (r <= row1) *reinterpret_cast<u32x4*>(op + 32 * k) = u32x4{lo[0], lo[1], hi2[0], hi2[1]};
+      }
+      if (t.lse != nullptr && grp == 0 && r <= row1) t.lse[at] = paged_lse(m_run[qh], l_tot[qh]);
     }
   }
 }
