@@ -590,7 +590,23 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 #pragma unroll
   for (int qh = 0; qh < kQH; ++qh) l_tot[qh] = 0.0f;
   if (n_tiles > 0) {
+    // One word per wave through LDS (the tiles are no longer read after the first barrier):
+    // what any wave found.
+    auto found = [&](bool overflow) __attribute__((always_inline)) {
+      const int mine = (__builtin_amdgcn_ballot_w64(overflow) != 0 ? 1 : 0) |
+                       (__builtin_amdgcn_ballot_w64(bad) != 0 ? 2 : 0);
+      __builtin_amdgcn_s_waitcnt(0);
+      __syncthreads();
+      int* flags = reinterpret_cast<int*>(lds);
+      if (lane == 0) flags[wave] = mine;
+      __syncthreads();
+      int all = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) all |= flags[w];
+      return all;
+    };
     bool checked_pass = t.lse != nullptr || (b.window >= 0 && !b.block);
+    int all = 0;
     if (!checked_pass) {
       key_loop(std::integral_constant<int, kPassFast>{});
       bool overflow = false;
@@ -606,20 +622,10 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
           for (int j = 0; j < 4; ++j) any = fmaf(o[dt][qh][j], 0.0f, any);
         overflow |= any != 0.0f;
       }
-      // One flag per wave through LDS (the tiles are no longer read after the first barrier;
-      // the last one keeps the flags until every wave has read them).
-      const bool mine = __builtin_amdgcn_ballot_w64(overflow) != 0;
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
-      int* flags = reinterpret_cast<int*>(lds);
-      if (lane == 0) flags[wave] = mine ? 1 : 0;
-      __syncthreads();
-      bool any = false;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) any |= flags[w] != 0;
-      __syncthreads();
-      checked_pass = any;
-      if (any) {
+      all = found(overflow);
+      checked_pass = (all & 1) != 0;
+      if (checked_pass) {
+        __syncthreads();   // (every wave has read the flags)
 #pragma unroll
         for (int dt = 0; dt < C::DT; ++dt)
 #pragma unroll
@@ -633,19 +639,11 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       key_loop(std::integral_constant<int, kPassChecked>{});
 #pragma unroll
       for (int qh = 0; qh < kQH; ++qh) l_tot[qh] = sum_across_groups(l_run[qh]);
+      all = found(false);
     }
 
     // V elements that clean_v kept out of the products, for the rows that see their key
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    int* flags = reinterpret_cast<int*>(lds);
-    const bool mine = __builtin_amdgcn_ballot_w64(bad) != 0;
-    if (lane == 0) flags[wave] = mine ? 1 : 0;
-    __syncthreads();
-    bool any = false;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) any |= flags[w] != 0;
-    if (any && rows_differ) {
+    if ((all & 2) != 0 && rows_differ) {
 #pragma unroll 1
       for (int n = 0; n < kBK * n_tiles; ++n) {
         const int key = blocks.key0(t_begin + n / kBK) + n % kBK;
