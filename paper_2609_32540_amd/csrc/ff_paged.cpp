@@ -121,15 +121,15 @@ struct Plan {
 // once.
 constexpr int kManyRows = 32;
 
-// Whether a bf16 batch runs on the kernel of few rows alone, by estimated times (us): that
-// kernel reads the keys once from HBM and again, mostly from L2, for every further tile of
-// 32 rows; the other takes equal time for its key blocks, one tile's at the least, and a
-// fixed part for prologue, partials and join, and for the first one's launch where it is
-// needed as well.  The constants are fits to 1 to 64
-// sequences x 48 to 256 rows x 300 to 30000 keys and to prompts of 20 to 2000 tokens, either
-// kernel forced: 2 sequences x 588 tokens over 2350 keys, 2 heads 24 against 34; 5 prompts of
-// up to 300 tokens, 5 heads 11 against 31; 8 x 48 rows x 4000 keys, 12 heads 80 against 55; 1170
-// tokens over 7000 keys, 12 heads 132 against 69.  Keys are counted by the table's columns.
+// Whether a bf16 batch runs on the kernel of few rows alone, by estimated times (us).  That
+// kernel reads the keys once from HBM, and again, mostly from L2, for every further tile of
+// 32 rows.  The other takes equal time for its key blocks, but one tile's at the least, and a
+// fixed part for prologue, partials and join, and for the first one's launch where that is
+// needed as well.  The constants are fits to 1 to 64 sequences x 48 to 256 rows x 300 to 30000
+// keys and to prompts of 20 to 2000 tokens, either kernel forced: 2 sequences x 588 tokens over
+// 2350 keys, 2 heads 24 against 34; 5 prompts of up to 300 tokens, 5 heads 11 against 31; 8 x 48
+// rows x 4000 keys, 12 heads 80 against 55; 1170 tokens over 7000 keys, 12 heads 132 against 69.
+// Keys are counted by the table's columns.
 bool few_rows_alone(const ff_paged_desc& d, int64_t rows, bool both, double keys, int cus) {
   const double seqs = std::min(d.n_seqs, d.n_tokens);
   const double key_bytes = 4.0 * d.head_dim * d.num_kv_heads;
@@ -187,8 +187,8 @@ Plan make_plan(const ff_paged_desc& d) {
     l.split.min_per = 8;
     // Parts for launches of fewer tiles than CUs.  From three quarters of them on there is
     // nothing to gain (two prompts of 5000 and 4000 tokens, 32/8 heads: 361 us with the join
-    // that finds no parts, 355 without; parts that even out the lengths of a causal batch
-    // cost more in partials than they save, below).
+    // that finds no parts, 355 without), and parts that even out tiles of unequal length cost
+    // more in partials than they save (spread 2 to 4 for a mixed batch: 142 us to 154 to 180).
     l.split.target = 4 * l.tiles * d.num_kv_heads >= 3 * cus ? 0 : std::max(cus / d.num_kv_heads, 1);
     l.split.spread = 0;
     set_items(d, &l, (keys + 63) / 64, l.split.min_per);

@@ -525,8 +525,9 @@ hipError_t launch_paged_join(int rows, int used, const PagedBatch& b, const Page
                              int dtype, hipStream_t stream) {
   // a workgroup for every 16 outputs of four elements, whose parts 16 groups of threads share
   // (one sequence of 12800 tokens, one head: 20.0 us in all with 2 outputs and as many groups
-  // as fit, 14.9 with 16, 15.5 with 32), up to two per CU, four for the 256-row tiles (12 sequences of 25 rows, 8 heads: 32.3 us
-  // with two, 34.3 with eight, since each workgroup looks its tile up)
+  // as fit, 14.9 with 16, 15.5 with 32), up to two per CU, four for the 256-row tiles (12
+  // sequences of 25 rows, 8 heads: 32.3 us with two, 34.3 with eight, since each workgroup looks
+  // its tile up)
   const int64_t groups = tiles * b.kv_heads;
   int64_t slices = (int64_t(used) * head_dim / 4 + 15) / 16;
   const int64_t most = ((rows > 32 ? 4 : 2) * device_cus() + groups - 1) / groups;
