@@ -165,8 +165,10 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 
   // The wave's blocks.  The rests of the probabilities meet a V element that is not finite as
   // 0 or a negative number, which would make an infinity NaN: a wave whose O is not finite
-  // goes over its blocks again without them.
+  // goes over its blocks again without them, and with weights of at most 1, so that values near
+  // the largest bf16 stay finite.
   for (bool rests = true;; rests = false) {
+    const float raise = rests ? kRaise : 0.0f;
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
       m_run[x] = -FLT_MAX;   // (finite: keys that score -inf get weight 0)
@@ -269,12 +271,12 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
         mx[x] = fmaxf(mx[x], fmaxf(fmaxf(s[1][x][0], s[1][x][1]), fmaxf(s[1][x][2], s[1][x][3])));
         mx[x] = max_across_groups(mx[x]) * t.scale_log2;
         // the first block's max is the reference from then on, until a score passes it far
-        over |= mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + kRaise);
+        over |= mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + raise);
       }
       if (__builtin_amdgcn_ballot_w64(over) != 0) {
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          const float m_new = mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + kRaise) ? mx[x] : m_run[x];
+          const float m_new = mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + raise) ? mx[x] : m_run[x];
           const float alpha = __builtin_amdgcn_exp2f(m_run[x] - m_new);
           l_run[x] *= alpha;
           m_run[x] = m_new;

@@ -370,6 +370,22 @@ def test_scores_far_apart(dtype):
     c.check_attention(rows=[0, 94, 394], block=True)
 
 
+@pytest.mark.parametrize("dtype,news,length,hk,form", [
+    (BF16, [1, 1], 700, 1, None), (BF16, [1], 9000, 1, None), (BF16, [20], 300, 1, None), (BF16, [700], 1000, 64, MANY),
+    (F32, [1, 1], 700, 1, None), (F32, [1], 9000, 1, None), (F32, [20], 300, 1, None)])
+def test_large_values_under_rising_scores(dtype, news, length, hk, form):
+    """V of 2^100 where scores end 43 log2 units above the first block's: a weight relative to that
+    block times V is past float32, the result is not."""
+    c = Case(news, [length] * len(news), dtype=dtype, d=64, hk=hk, group=1, page=64)
+    c.q[:, :, 0] = 8.0
+    for s in range(len(news)):
+        for j in range(length):
+            p, sl = c.b.place(s, j)
+            c.k_pages[p, :, sl, 0] = 30.0 * j / length
+    c.v_pages *= 2.0 ** 100
+    c.check_attention(rows=[0, sum(news) - 1], heads=[0, hk - 1], max_new=news[0], min_new=news[0], form=form)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_scores_of_minus_infinity_weigh_nothing(dtype):
     c = Case([1, 20], [100, 60], dtype=dtype, hk=1, group=1, d=64)
