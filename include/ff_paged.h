@@ -102,7 +102,7 @@ typedef struct {
  * NULL) are the t, h and w positions of each row; NULL turns every axis by the token's
  * index i (text).  Angles, cosines, sines and the rotation are evaluated in float64 and
  * rounded once to dtype (nearest even); V is copied bit for bit.  The tensors must not
- * overlap the pool.  One kernel launch. */
+ * overlap the pool.  One kernel launch of at most 2^24 - 1 rows. */
 ff_status ff_paged_append(const ff_paged_desc* desc, const ff_paged_rope* rope, const void* q,
                           const void* k, const void* v, int64_t q_stride, int64_t k_stride,
                           int64_t v_stride, const int32_t* positions, void* q_out, void* k_pages,

@@ -238,6 +238,9 @@ ff_status ff_paged_append(const ff_paged_desc* desc, const ff_paged_rope* rope, 
   if (!(r.rope_theta > 0.0) || !std::isfinite(r.rope_theta))
     return fail(FF_ERR_INVALID_ARG, "rope_theta must be positive");
   if (d.n_seqs == 0 || d.n_tokens == 0) return ok();
+  // (a grid holds at most 2^32 - 1 threads)
+  if (d.n_tokens > int64_t(UINT32_MAX) / 256)
+    return fail(FF_ERR_UNSUPPORTED, "too many rows for one launch");
   if ((st = check_rows(d, k, k_stride, d.num_kv_heads, "k")) != FF_OK) return st;
   if ((st = check_rows(d, v, v_stride, d.num_kv_heads, "v")) != FF_OK) return st;
   if (q) {
@@ -265,18 +268,7 @@ ff_status ff_paged_append(const ff_paged_desc* desc, const ff_paged_rope* rope, 
   a.v_stride = v_stride;
   a.n_t = r.rope_pairs_t;
   a.n_th = r.rope_pairs_t + r.rope_pairs_h;
-  // (64 powers take longer than the rest of the call: kept for the next call of this rotation)
-  struct Memo {
-    ff_paged_rope rope;
-    double omega[64];
-  };
-  static thread_local Memo memo = {};
-  if (memo.rope.rope_pairs_t != r.rope_pairs_t || memo.rope.rope_pairs_h != r.rope_pairs_h ||
-      memo.rope.rope_pairs_w != r.rope_pairs_w || memo.rope.rope_theta != r.rope_theta) {
-    ff::rope_frequencies(r.rope_pairs_t, r.rope_pairs_h, r.rope_pairs_w, r.rope_theta, memo.omega);
-    memo.rope = r;
-  }
-  std::memcpy(a.omega, memo.omega, sizeof(a.omega));
+  ff::rope_frequencies(r.rope_pairs_t, r.rope_pairs_h, r.rope_pairs_w, r.rope_theta, a.omega);
   return hip_status(ff::launch_paged_append(make_batch(d), a, d.head_dim, d.dtype,
                                             static_cast<hipStream_t>(stream)),
                     "paged_append launch");

@@ -577,7 +577,10 @@ def packed_attention_bwd_static(q, k, v, out, dout, lse, dq, dk, dv, d_anchor_k=
 _PAGED_DTYPES = {torch.bfloat16: FF_DT_BF16, torch.float32: FF_DT_F32}
 
 
-def _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table) -> Exception:
+_INT32_MAX = 2 ** 31 - 1
+
+
+def _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new) -> Exception:
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages"), (q_start, "q_start"),
                     (kv_len, "kv_len"), (page_table, "page_table")):
         if not isinstance(t, torch.Tensor):
@@ -598,6 +601,10 @@ def _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table) -> Exception:
     n = kv_len.numel()
     if kv_len.dim() != 1 or q_start.shape != (n + 1,) or page_table.dim() != 2 or page_table.shape[0] != n:
         return ValueError("kv_len must be [n_seqs], q_start [n_seqs + 1], page_table [n_seqs][max_pages]")
+    if dev.type != "cuda":
+        return ValueError(f"the pool is on {dev}, expected a GPU")
+    if max(min_new, max_new) > _INT32_MAX:
+        return ValueError("min_new and max_new must fit in 32 bits")
     return ValueError("kv_len, q_start and the rows of page_table must be contiguous")
 
 
@@ -614,12 +621,13 @@ def _paged_desc(q_heads: int, n_tokens: int, k_pages: torch.Tensor, v_pages: tor
                 and kv_len.dtype is i32 and q_start.dtype is i32 and page_table.dtype is i32
                 and kv_len.get_device() == dev and q_start.get_device() == dev
                 and page_table.get_device() == dev and n_starts == n_seqs + 1 and n_rows == n_seqs
-                and kv_len.is_contiguous() and q_start.is_contiguous() and (unit == 1 or max_pages <= 1))
+                and kv_len.is_contiguous() and q_start.is_contiguous() and (unit == 1 or max_pages <= 1)
+                and dev >= 0 and min_new <= _INT32_MAX and max_new <= _INT32_MAX)
         dtype = _PAGED_DTYPES[dt]
     except (ValueError, TypeError, AttributeError, KeyError):
         good = False
     if not good:
-        raise _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table)
+        raise _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new)
     return PagedDesc(num_pages, page_tokens, q_heads, kv_heads, d, dtype, n_seqs, n_tokens, max_pages,
                      min_new, max_new, 0, stride if n_seqs > 1 else max_pages, q_start.data_ptr(),
                      kv_len.data_ptr(), page_table.data_ptr())
@@ -725,6 +733,8 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     """
     qp, qs, n, heads = _rows(q, k_pages, "q")
     desc = _paged_desc(heads, n, k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new)
+    if max(abs(window), abs(anchor_tokens)) > _INT32_MAX:
+        raise ValueError("window and anchor_tokens must fit in 32 bits")
     dev = q.device
     if out is None:
         out = _empty_on(q, stream)

@@ -142,6 +142,26 @@ def test_binding_refusals():
             app(**bad)
 
 
+def test_rows_of_one_append():
+    """One launch: a thread count of 32 bits, 256 for a row."""
+    assert append(desc(n_tokens=2 ** 24), k=None) == 5
+    assert append(desc(n_tokens=2 ** 24 - 1), k=None) == 1    # (past that check: k is missing)
+
+
+@pytest.mark.parametrize("hint", [dict(min_new=2 ** 31), dict(max_new=2 ** 32 + 1), {}])
+def test_binding_refuses_host_memory_and_wide_hints(hint):
+    """A batch in host memory is good in everything but its place; the hints are looked at after it."""
+    i32 = dict(dtype=torch.int32)
+    kp, q = torch.zeros((4, 2, 16, 128), dtype=torch.bfloat16), torch.zeros((1, 8, 128), dtype=torch.bfloat16)
+    batch = torch.tensor([0, 1], **i32), torch.tensor([5], **i32), torch.zeros((1, 2), **i32)
+    with pytest.raises(ValueError, match="GPU"):
+        ff.paged_attention(q, kp, kp, *batch, **hint)
+    with pytest.raises(ValueError, match="GPU"):
+        ff.paged_attention_workspace(q, kp, *batch, **hint)
+    with pytest.raises(ValueError, match="GPU"):
+        ff.paged_append(q[:, :2], q[:, :2], kp, kp, *batch, q=q)
+
+
 def test_reference_against_the_oracle():
     """One sequence whose pages are in order: causal and block attention, and the rotation."""
     rng = np.random.default_rng(1)
