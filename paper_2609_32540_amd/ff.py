@@ -633,17 +633,28 @@ def _paged_desc(q_heads: int, n_tokens: int, k_pages: torch.Tensor, v_pages: tor
                      kv_len.data_ptr(), page_table.data_ptr())
 
 
-def _rows(t: torch.Tensor, like: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
+def _pool(k_pages: torch.Tensor) -> Tuple[torch.dtype, int, int]:
+    """(dtype, device index, head dim) that a call's tensors share."""
+    if not isinstance(k_pages, torch.Tensor):
+        raise TypeError("k_pages must be a torch.Tensor")
+    shape = k_pages.shape
+    if len(shape) != 4:
+        raise ValueError("k_pages and v_pages must be [num_pages][kv heads][page tokens][d]")
+    return k_pages.dtype, k_pages.get_device(), shape[3]
+
+
+def _rows(t: torch.Tensor, pool: Tuple[torch.dtype, int, int], name: str) -> Tuple[int, int, int, int]:
     """(pointer, elements between rows, rows, heads) of [n_tokens][heads][d] rows of heads, each
     dense."""
-    if not isinstance(t, torch.Tensor) or not isinstance(like, torch.Tensor):
-        raise TypeError(f"{name} and the pool must be torch.Tensors")
-    d = like.shape[-1]
-    if t.dim() != 3 or t.size(2) != d:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [n_tokens][heads][{d}]")
-    if t.dtype is not like.dtype or t.get_device() != like.get_device():
-        raise ValueError(f"{name} must be {like.dtype} on {like.device} (got {t.dtype} on {t.device})")
-    rows, heads = t.size(0), t.size(1)
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    dtype, dev, d = pool
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != d:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected [n_tokens][heads][{d}]")
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} is {t.dtype} on {t.device}, the pool {dtype} on device {dev}")
+    rows, heads, _ = shape
     row, head, unit = t.stride()
     if unit != 1 or (head != d and heads > 1):
         raise ValueError(f"the heads of a row of {name} must be contiguous")
@@ -651,9 +662,9 @@ def _rows(t: torch.Tensor, like: torch.Tensor, name: str) -> Tuple[int, int, int
     return t.data_ptr(), row if rows > 1 else heads * d, rows, heads
 
 
-def _like(t: torch.Tensor, q: torch.Tensor, name: str) -> int:
-    """Pointer of a dense tensor of q's shape, dtype and device."""
-    if t.shape != q.shape or t.dtype != q.dtype or t.get_device() != q.get_device() or not t.is_contiguous():
+def _like(t: torch.Tensor, q: torch.Tensor, pool: Tuple[torch.dtype, int, int], name: str) -> int:
+    """Pointer of a dense tensor of q's shape, in the pool's dtype and device."""
+    if t.shape != q.shape or t.dtype is not pool[0] or t.get_device() != pool[1] or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {q.dtype} tensor of shape {tuple(q.shape)} on {q.device}")
     return t.data_ptr()
 
@@ -684,20 +695,21 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_page
     Returns the rotated q (q_out, or a new tensor whose rows of no token are undefined),
     None without q.
     """
-    kp, ks, n, heads = _rows(k, k_pages, "k")
-    vp, vs, v_rows, v_heads = _rows(v, k_pages, "v")
+    pool = _pool(k_pages)
+    kp, ks, n, heads = _rows(k, pool, "k")
+    vp, vs, v_rows, v_heads = _rows(v, pool, "v")
     if v_rows != n or v_heads != heads or heads != k_pages.shape[1]:
         raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} must have one shape and the pool's "
                          f"{k_pages.shape[1]} heads")
     qp = qop = None
     qs = 0
     if q is not None:
-        qp, qs, q_rows, heads = _rows(q, k_pages, "q")
+        qp, qs, q_rows, heads = _rows(q, pool, "q")
         if q_rows != n:
             raise ValueError(f"q has {q_rows} rows, k {n}")
         if q_out is None:
             q_out = _empty_on(q, stream)
-        qop = _like(q_out, q, "q_out")
+        qop = _like(q_out, q, pool, "q_out")
     elif q_out is not None:
         raise ValueError("q_out without q")
     pp = None
@@ -731,14 +743,15 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     base-2 log-sum-exp.  Rows of no sequence keep what `out` holds (a new `out`: undefined).
     workspace: a uint8 tensor of paged_attention_workspace() bytes, default a new one.
     """
-    qp, qs, n, heads = _rows(q, k_pages, "q")
+    pool = _pool(k_pages)
+    qp, qs, n, heads = _rows(q, pool, "q")
     desc = _paged_desc(heads, n, k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new)
     if max(abs(window), abs(anchor_tokens)) > _INT32_MAX:
         raise ValueError("window and anchor_tokens must fit in 32 bits")
     dev = q.device
     if out is None:
         out = _empty_on(q, stream)
-    op = _like(out, q, "out")
+    op = _like(out, q, pool, "out")
     lp = _dense(lse, (n, heads), torch.float32, dev, "lse") if lse is not None else None
     if scale is None:
         scale = 1.0 / math.sqrt(q.shape[2])
@@ -762,7 +775,7 @@ def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, q_start: t
                               kv_len: torch.Tensor, page_table: torch.Tensor, *, min_new: int = 0,
                               max_new: int = 0) -> int:
     """ff_paged_attention_workspace: workspace bytes of a paged_attention call (sizes only)."""
-    _, _, n, heads = _rows(q, k_pages, "q")
+    _, _, n, heads = _rows(q, _pool(k_pages), "q")
     desc = _paged_desc(heads, n, k_pages, k_pages, q_start, kv_len, page_table, min_new, max_new)
     bytes_ = _call_on(q.device.index, lib().ff_paged_attention_workspace, ctypes.byref(desc))
     if bytes_ == 0 and lib().ff_last_error():
