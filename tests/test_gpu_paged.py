@@ -107,6 +107,15 @@ def test_decode_lengths(dtype, d, hk, group):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("group", [31, 71, 300])
+@pytest.mark.parametrize("news", [[1, 1, 1], [1, 5, 2]])
+def test_one_kv_head_for_many_query_heads(dtype, group, news):
+    """A token's heads in several tiles, tiles that begin inside a token."""
+    for window in (-1, 100):
+        Case(news, [900, 20, 300], dtype=dtype, d=64, hk=1, group=group).check_attention(window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 def test_decode_page_sizes(dtype, page):
     Case([1, 1, 1], [page - 1, 3 * page + 5, 611], dtype=dtype, page=page).check_attention(max_new=1)
@@ -465,6 +474,27 @@ def test_offsets_past_32_bits():
     assert torch.equal(vp[pages[4], :, at], k[0])
     want = ref.rotate(ref.f64(k[0]), [length - 1] * 3, ref.rope_split(d), 10000.0)
     assert (np.abs(ref.f64(kp[pages[4], :, at]) - want) <= ref.U_BF16 * np.abs(want) + 1e-9).all()
+
+
+@pytest.mark.parametrize("dtype,news,group", [(BF16, 600, 4), (F32, 1, 2)])
+def test_offsets_past_32_bits_of_the_other_kernels(dtype, news, group):
+    hk, page, d, length = 16, 256, 128, 1100
+    n_pages = 2 ** 32 // (hk * page * d) + 40
+    kp = torch.empty((n_pages, hk, page, d), dtype=dtype, device=DEV)
+    vp = torch.empty_like(kp)
+    pages = [n_pages - 1, 3, n_pages - 7, 0, n_pages - 2]
+    small = Case([news], [length], dtype=dtype, hk=hk, group=group, page=page)
+    for c, p in enumerate(pages):
+        at = int(small.b.table[0, c])
+        kp[p] = small.k_pages[at].to(DEV)
+        vp[p] = small.v_pages[at].to(DEV)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    qs, kl, tb = torch.tensor([0, news], **i32), torch.tensor([length], **i32), torch.tensor([pages], **i32)
+    rows, heads = [0, news // 2, news - 1], [0, hk * group - 1]
+    got = ref.f64(ff.paged_attention(small.q.to(DEV), kp, vp, qs, kl, tb, min_new=news))
+    assert dtype == F32 or forms()[2] == 256
+    r = ref.attention(small.b, small.q, small.k_pages, small.v_pages, rows=rows, heads=heads)
+    assert (np.abs(got - r.out) <= r.tol)[rows][:, heads].all()
 
 
 # ---- append ------------------------------------------------------------------------
