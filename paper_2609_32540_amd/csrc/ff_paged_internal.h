@@ -53,10 +53,11 @@ __device__ inline void paged_copy(uint32_t dst, const char* base, const uint32_t
   else
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\t"
                  "global_load_lds_dwordx4 %1, %5 nt\n\t"
-                 "global_load_lds_dwordx4 %2, %5 offset:1024 nt\n\t"
-                 "global_load_lds_dwordx4 %3, %5 offset:2048 nt\n\t"
-                 "global_load_lds_dwordx4 %4, %5 offset:3072 nt"
-                 :: "s"(dst), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base) : "memory");
+                 "global_load_lds_dwordx4 %2, %5 offset:%6 nt\n\t"
+                 "global_load_lds_dwordx4 %3, %5 offset:%7 nt\n\t"
+                 "global_load_lds_dwordx4 %4, %5 offset:%8 nt"
+                 :: "s"(dst), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(base),
+                    "n"(1 * 1024), "n"(2 * 1024), "n"(3 * 1024) : "memory");
 }
 
 constexpr int kPagedPromptRows = 256;   // rows of a tile of launch_paged_prompt
