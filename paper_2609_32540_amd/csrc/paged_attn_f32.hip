@@ -9,10 +9,11 @@
 // four products of each query tile.  The max is subtracted from a score before the factor
 // log2 e is applied: the largest key's exponent is then exactly 0.
 //
-// One new token each of 16 sequences of up to 2300 tokens, 12 heads x 128: 57 us with the
-// join = 4.1 TB/s (bound by HBM; workgroups of eight waves, one per CU instead of two, 63 us);
-// one block of 2184 tokens over 8700 keys, 3 heads: 331 us = 88 TFLOP/s (the float32 matrix
-// rate, 153 TFLOP/s in a large product).
+// One new token each of 16 sequences of up to 2300 tokens, 12 heads x 128: 54 us with the
+// join = 4.3 TB/s (bound by HBM; workgroups of eight waves, one per CU instead of two, 6 us more);
+// one block of 2184 tokens over 8700 keys, 3 heads: 300 us = 98 TFLOP/s (the float32 matrix
+// rate, 153 TFLOP/s in a large product; the matrix unit is busy 62% of the time, as the softmax
+// of a wave and the other wave's products hardly overlap).
 
 #include <hip/hip_runtime.h>
 
@@ -95,24 +96,31 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   };
   const float* kpool = static_cast<const float*>(t.k_pages);
   const float* vpool = static_cast<const float*>(t.v_pages);
-  // (past the caches where no other workgroup reads the key)
-  auto load = [](const float* p) __attribute__((always_inline)) {
-    const f32x4* v = reinterpret_cast<const f32x4*>(p);
+  // 16 bytes per lane from a scalar base (the compiler would make vector addresses of the pool's
+  // start and add to those); past the caches where no other workgroup reads the key
+  using Base = const __attribute__((address_space(1))) char*;
+  auto base_of = [](const float* p) __attribute__((always_inline)) {
+    Base base = (Base)p;
+    asm volatile("" : "+s"(base));
+    return base;
+  };
+  auto load = [](Base base, uint32_t bytes) __attribute__((always_inline)) {
+    const auto* v = (const __attribute__((address_space(1))) f32x4*)(base + bytes);
     return NT ? __builtin_nontemporal_load(v) : *v;
   };
   f32x4 kreg[KT], vreg[4][VH];
+  const uint32_t k_lane = 4 * (l16 * D + 4 * grp), v_lane = 4 * (4 * grp * D + 4 * l16);   // bytes from a scalar base
   auto load_k = [&](int64_t off) __attribute__((always_inline)) {
-    const float* p = kpool + off + l16 * D + 4 * grp;
+    const Base p = base_of(kpool + off);
 #pragma unroll
-    for (int i = 0; i < KT; ++i) kreg[i] = load(p + 16 * i);
+    for (int i = 0; i < KT; ++i) kreg[i] = load(p + 64 * i, k_lane);
   };
   auto load_v = [&](int64_t off) __attribute__((always_inline)) {
+    const Base p = base_of(vpool + off);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float* p = vpool + off + (4 * grp + j) * D + 4 * l16;
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int h = 0; h < VH; ++h) vreg[j][h] = load(p + 64 * h);
-    }
+      for (int h = 0; h < VH; ++h) vreg[j][h] = load(p + 4 * (j * D + 64 * h), v_lane);
   };
 
   int tb = t0 + wave, i = 0;
@@ -121,10 +129,14 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   if (tb < t1) {
     load_pages(0);
     page = __builtin_amdgcn_readlane(page_of, 0);
-    off = block_offset(page, blocks.key0(tb));
+    off = uniform(block_offset(page, blocks.key0(tb)));
     load_k(off);
+    // (V behind K: the loop waits for K with V's loads in flight)
+    __builtin_amdgcn_sched_barrier(0);
     load_v(off);
   }
+  // Every turn issues the same loads in the same order, K of the next block, then its V (behind
+  // the last one of page 0): so the waits for K leave V's loads in flight and the other way round.
   while (tb < t1) {
     f32x4 s[QT];
 #pragma unroll
@@ -141,12 +153,14 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     // the next block: its K now, its V once this block's V is consumed
     tb += kWaves;
     ++i;
+    off = 0;
     if (tb < t1) {
       if ((i & 63) == 0) load_pages(i);
       page = __builtin_amdgcn_readlane(page_of, i & 63);
-      off = block_offset(page, blocks.key0(tb));
-      load_k(off);
+      off = uniform(block_offset(page, blocks.key0(tb)));
     }
+    load_k(off);
+    __builtin_amdgcn_sched_barrier(0);
 
     const bool edge = j0 + kBK > head_r.hi || cur < 0 || (j0 < tail_r.lo && j0 + kBK > b.anchor_tokens);
     bool spread = false;
@@ -245,7 +259,9 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
         }
       }
     }
-    if (tb < t1) load_v(off);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(off);
+    __builtin_amdgcn_sched_barrier(0);
   }
 
   // join the waves
