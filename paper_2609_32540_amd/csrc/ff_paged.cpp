@@ -141,6 +141,24 @@ bool few_rows_alone(const ff_paged_desc& d, int64_t rows, bool both, double keys
   return few <= many;
 }
 
+// Parts of each of `tiles` float32 tiles of 32 rows of long prompts, which the matrix unit
+// bounds: a CU runs a whole number of parts, and every part adds 5 us, the join 6.  Against as
+// many parts as make two items per CU: 188 tiles over 4500 keys 186 us and 150 (4 parts each
+// instead of 2), 207 over 8700 339 and 303, 350 over 1100 340 and 236.
+int parts_of_f32_tiles(const ff_paged_desc& d, int64_t tiles, double keys, int cus) {
+  const double tile = keys / 64 * (d.head_dim == 128 ? 2.4 : 1.3);   // us on one CU
+  int best = 1;
+  double least = 0;
+  for (int p = 1; p <= 16; ++p) {
+    const double us = double((tiles * p + cus - 1) / cus) * (tile / p + 5.0) + (p > 1 ? 6.0 : 0.0);
+    if (p == 1 || us < least) {
+      best = p;
+      least = us;
+    }
+  }
+  return best;
+}
+
 // blocks: of the longest sequence; none is cut that has no more than `whole` of them
 void set_items(const ff_paged_desc& d, Launch* l, int64_t blocks, int64_t whole) {
   if (blocks <= whole) l->split.target = 0;
@@ -172,6 +190,13 @@ Plan make_plan(const ff_paged_desc& d) {
     l.split.min_per = 256 / block;
     l.split.target = (2 * cus + d.num_kv_heads - 1) / d.num_kv_heads;
     l.split.spread = l.tiles * d.num_kv_heads <= 16 * cus ? (bf16 ? 4 : 2) : 0;
+    // (fewer tiles per sequence are bound by the keys' bytes: 10 sequences of 48 rows over up to
+    // 23000 keys 93 us by this rule, 54 without)
+    if (!bf16 && rows >= 4 * int64_t(l.rows) * d.n_seqs) {
+      const int parts = parts_of_f32_tiles(d, l.tiles * d.num_kv_heads, double(keys), cus);
+      l.split.target = parts > 1 ? 1 : 0;
+      l.split.spread = parts + 1;
+    }
     set_items(d, &l, (keys + block - 1) / block, 1024 / block);
     // Short caches in more workgroups than two per CU: two waves each (no more of their
     // blocks than two waves' copies cover are left for four), twice as many sequences at once.
