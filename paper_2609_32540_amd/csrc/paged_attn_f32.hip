@@ -29,6 +29,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kBK = 16;                   // keys per block
 constexpr float kLog2e = 1.44269504f;
+constexpr float kRaise = 4.0f;            // natural units a score may pass the reference by: every
+                                          // row's running max would move some row's O in most blocks
 
 template <int D, int QT, bool NT>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -198,23 +200,23 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     }
 
     bool raised = false;
-    float alpha[QT];
+    float mx[QT];
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
-      float mx = fmaxf(fmaxf(s[x][0], s[x][1]), fmaxf(s[x][2], s[x][3]));
-      mx = fmaxf(m_run[x], max_across_groups(mx));
-      alpha[x] = __builtin_amdgcn_exp2f((m_run[x] - mx) * kLog2e);
-      raised |= mx != m_run[x];
-      m_run[x] = mx;
+      mx[x] = max_across_groups(fmaxf(fmaxf(s[x][0], s[x][1]), fmaxf(s[x][2], s[x][3])));
+      raised |= mx[x] > m_run[x] + kRaise;   // (-FLT_MAX + kRaise is -FLT_MAX)
     }
     if (__builtin_amdgcn_ballot_w64(raised) != 0) {
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        l_run[x] *= alpha[x];
+        const float m_new = mx[x] > m_run[x] + kRaise ? mx[x] : m_run[x];
+        const float alpha = __builtin_amdgcn_exp2f((m_run[x] - m_new) * kLog2e);
+        m_run[x] = m_new;
+        l_run[x] *= alpha;
 #pragma unroll
         for (int h = 0; h < VH; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[x][h][e] *= alpha[x];
+          for (int e = 0; e < 4; ++e) o[x][h][e] *= alpha;
       }
     }
 #pragma unroll
