@@ -142,16 +142,20 @@ bool few_rows_alone(const ff_paged_desc& d, int64_t rows, bool both, double keys
 }
 
 // Parts of each of `tiles` float32 tiles of 32 rows of long prompts, which the matrix unit
-// bounds: a CU runs a whole number of parts, and every part adds 5 us, the join 6.  Against as
-// many parts as make two items per CU: 188 tiles over 4500 keys 186 us and 150 (4 parts each
-// instead of 2), 207 over 8700 339 and 303, 350 over 1100 340 and 236.
+// bounds: a CU runs a whole number of parts, every part adds 5 us, and the join 6 and the
+// partials' way to HBM and back (5 TB/s).  Against as many parts as make two items per CU: 188
+// tiles over 4500 keys 186 us and 150 (4 parts each instead of 2), 207 over 8700 339 and 303.
+// The keys are cut for a gain of 3% and more, which many rounds of tiles do not leave, and into
+// at most 16 items per CU, so that the workspace stays within 70 MB (256 CUs).
 int parts_of_f32_tiles(const ff_paged_desc& d, int64_t tiles, double keys, int cus) {
   const double tile = keys / 64 * (d.head_dim == 128 ? 2.4 : 1.3);   // us on one CU
+  const double moved = double(tiles) * ff::paged_part_floats(32, d.head_dim) * 4 * 2 / 5e6;   // us per part
   int best = 1;
-  double least = 0;
-  for (int p = 1; p <= 16; ++p) {
-    const double us = double((tiles * p + cus - 1) / cus) * (tile / p + 5.0) + (p > 1 ? 6.0 : 0.0);
-    if (p == 1 || us < least) {
+  double least = 0.97 * double((tiles + cus - 1) / cus) * (tile + 5.0);
+  // (p + 1 parts of a tile bound the items of a ragged batch)
+  for (int p = 2; p <= 16 && tiles * (p + 1) <= 16 * cus; ++p) {
+    const double us = double((tiles * p + cus - 1) / cus) * (tile / p + 5.0) + 6.0 + p * moved;
+    if (us < least) {
       best = p;
       least = us;
     }
