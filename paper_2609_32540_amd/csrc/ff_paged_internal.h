@@ -72,16 +72,18 @@ __device__ inline uint32_t bf16_pair_finite(uint32_t w) {
   return w;
 }
 
-// Floats of one partial result: O [rt][d], then the reference and the sum of each row.
+// Floats of one partial result: the output [rt][d] of its keys alone, then the reference and the
+// sum of the weights of each row.  Parts are joined as the convex combination of their outputs, as
+// are the waves of a workgroup: sums of weighted values that are not yet divided would pass
+// float32's range where values are near its end.
 __host__ __device__ inline int64_t paged_part_floats(int rt, int d) { return int64_t(rt) * (d + 2); }
 
-// N elements of a row of the output; a row that saw nothing (l = 0) is zero
+// 1 / l, 0 for the sum of a row that saw nothing
+__device__ inline float paged_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+// N elements of a row of the output
 template <class T, int N>
-__device__ inline void paged_store(T* out, const float* acc, float l) {
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  float v[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = l == 0.0f ? 0.0f : acc[i] * inv;
+__device__ inline void paged_store(T* out, const float* v) {
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
     for (int i = 0; i < N; i += 4) {

@@ -2,14 +2,14 @@
 // length is split over workgroups and over the waves of a workgroup, and joined.
 //
 // Mathematics.  out = sum_j p_j v_j / sum_j p_j with p_j = 2^(c q.k_j - m), c = scale
-// log2 e.  Any split of the keys works with a reference m of its own: parts (O, m, l) join
-// as O = sum_w 2^(m_w - M) O_w, l likewise, M = max m_w.
+// log2 e.  Any split of the keys works with a reference m of its own: waves, and parts, join as
+// out = sum_w (2^(m_w - M) l_w / l) out_w, l = sum_w 2^(m_w - M) l_w, M = max m_w.
 //
 // Work split.  The query heads of one kv head read the same keys, so a tile is 16 QT rows
 // (token, query head of the group) of one sequence and kv head.  An item is a tile and one
 // of its parts of the keys (paged_plan.h); a workgroup of four waves runs one item of one
 // kv head, 32-key blocks dealt round robin to its waves, which join through LDS; items of
-// a tile with several parts leave unnormalised float32 partials in the workspace, joined
+// a tile with several parts leave float32 partial results in the workspace, joined
 // by paged_join_kernel.  What bounds it: every key and value is read from HBM once, while
 // the products fill the matrix unit's 16 columns with as few as one row.
 //
@@ -377,17 +377,20 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     float m = part_m[r];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w * C::kRows + r]);
-    float l = 0.0f;
-    f32x4 acc[2] = {};
+    float l = 0.0f, a[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const int row = w * C::kRows + r;
-      const float a = __builtin_amdgcn_exp2f(part_m[row] - m);
-      l += a * part_l[row];
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        acc[x] += a * *reinterpret_cast<const f32x4*>(part + row * C::kPitch + 8 * c + 4 * x);
+      a[w] = __builtin_amdgcn_exp2f(part_m[w * C::kRows + r] - m);
+      l += a[w] * part_l[w * C::kRows + r];
     }
+    const float inv = paged_inverse(l);
+    f32x4 acc[2] = {};
+    if (l != 0.0f)   // (a row that saw nothing is zero)
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          acc[x] += (a[w] * inv) * *reinterpret_cast<const f32x4*>(part + (w * C::kRows + r) * C::kPitch + 8 * c + 4 * x);
     if (it.parts > 1) {
       *reinterpret_cast<f32x4*>(ws + r * D + 8 * c) = acc[0];
       *reinterpret_cast<f32x4*>(ws + r * D + 8 * c + 4) = acc[1];
@@ -399,8 +402,7 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       const int tau = paged_token(b, row0 + r);
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
                          (row0 + r - tau * b.group);
-      paged_store<__bf16, 8>(static_cast<__bf16*>(t.out) + at * D + 8 * c,
-                             reinterpret_cast<const float*>(acc), l);
+      paged_store<__bf16, 8>(static_cast<__bf16*>(t.out) + at * D + 8 * c, reinterpret_cast<const float*>(acc));
       if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m, l);
     }
   }
@@ -464,15 +466,19 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
         float m_new = m;
 #pragma unroll
         for (int k = 0; k < 4; ++k) m_new = fmaxf(m_new, p + k * groups < it.parts ? pm[k] : m_new);
-        const float a = __builtin_amdgcn_exp2f((m - m_new) * kUnit);
-        l *= a;
-        acc *= a;
+        const float before = l * __builtin_amdgcn_exp2f((m - m_new) * kUnit);
+        l = before;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {   // pl becomes the part's weight
+          pl[k] = p + k * groups < it.parts ? pl[k] * __builtin_amdgcn_exp2f((pm[k] - m_new) * kUnit) : 0.0f;
+          l += pl[k];
+        }
+        const float inv = paged_inverse(l);
+        acc *= before * inv;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           if (p + k * groups >= it.parts) break;
-          const float w = __builtin_amdgcn_exp2f((pm[k] - m_new) * kUnit);
-          l += w * pl[k];
-          acc += w * pa[k];
+          acc += (pl[k] * inv) * pa[k];
         }
         m = m_new;
       }
@@ -484,12 +490,13 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
       if (g == 0) {
         for (int k = 1; k < groups; ++k) m = fmaxf(m, m_s[threadIdx.x + k * n]);
         l = 0.0f;
+        for (int k = 0; k < groups; ++k)
+          l += l_s[threadIdx.x + k * n] * __builtin_amdgcn_exp2f((m_s[threadIdx.x + k * n] - m) * kUnit);
+        const float inv = paged_inverse(l);
         acc = f32x4{};
         for (int k = 0; k < groups; ++k) {
           const int x = threadIdx.x + k * n;
-          const float w = __builtin_amdgcn_exp2f((m_s[x] - m) * kUnit);
-          l += w * l_s[x];
-          acc += w * acc_s[x];
+          acc += (l_s[x] * __builtin_amdgcn_exp2f((m_s[x] - m) * kUnit) * inv) * acc_s[x];
         }
       }
       __syncthreads();
@@ -498,7 +505,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedBatch b, 
       const int row = it.tile * RT + r, tau = paged_token(b, row);
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
                          (row - tau * b.group);
-      paged_store<T, 4>(static_cast<T*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc), l);
+      paged_store<T, 4>(static_cast<T*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc));
       if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m * kUnit, l);
     }
   }

@@ -292,14 +292,18 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     float m = part_m[r];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part_m[w * kRows + r]);
-    float l = 0.0f;
-    f32x4 acc = {};
+    float l = 0.0f, a[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float a = __builtin_amdgcn_exp2f((part_m[w * kRows + r] - m) * kLog2e);
-      l += a * part_l[w * kRows + r];
-      acc += a * *reinterpret_cast<const f32x4*>(part + (w * kRows + r) * kPitch + 4 * c);
+      a[w] = __builtin_amdgcn_exp2f((part_m[w * kRows + r] - m) * kLog2e);
+      l += a[w] * part_l[w * kRows + r];
     }
+    const float inv = paged_inverse(l);
+    f32x4 acc = {};
+    if (l != 0.0f)   // (a row that saw nothing is zero)
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+        acc += (a[w] * inv) * *reinterpret_cast<const f32x4*>(part + (w * kRows + r) * kPitch + 4 * c);
     if (it.parts > 1) {
       *reinterpret_cast<f32x4*>(ws + r * D + 4 * c) = acc;
       if (c == 0) {
@@ -310,8 +314,7 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       const int tau = paged_token(b, row0 + r);
       const int64_t at = int64_t(it.seq.q0 + tau) * (b.kv_heads * b.group) + head * b.group +
                          (row0 + r - tau * b.group);
-      paged_store<float, 4>(static_cast<float*>(t.out) + at * D + 4 * c,
-                            reinterpret_cast<const float*>(&acc), l);
+      paged_store<float, 4>(static_cast<float*>(t.out) + at * D + 4 * c, reinterpret_cast<const float*>(&acc));
       if (t.lse != nullptr && c == 0) t.lse[at] = paged_lse(m * kLog2e, l);
     }
   }

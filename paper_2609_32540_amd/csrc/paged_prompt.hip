@@ -678,21 +678,21 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 #pragma unroll
   for (int qh = 0; qh < kQH; ++qh) {
     const int r = q0 + 16 * qh + l16;
+    // a row that saw nothing (l = 0) is zero
+    const float inv = 1.0f / l_tot[qh];
+    const bool some = l_tot[qh] != 0.0f;
     if (it.parts > 1) {
       if (r > row1) continue;
       float* ws = t.part + (int64_t(item) * b.kv_heads + head) * paged_part_floats(kBlockQ, D);
       const int row = r - row0;
 #pragma unroll
       for (int dt = 0; dt < C::DT; ++dt)
-        *reinterpret_cast<f32x4*>(ws + row * D + 16 * dt + 4 * grp) = o[dt][qh];
+        *reinterpret_cast<f32x4*>(ws + row * D + 16 * dt + 4 * grp) = some ? o[dt][qh] * inv : f32x4{};
       if (grp == 0) {
         ws[kBlockQ * D + row] = m_run[qh];
         ws[kBlockQ * D + kBlockQ + row] = l_tot[qh];
       }
     } else {
-      // a row that saw nothing (l = 0) is zero
-      const float inv = 1.0f / l_tot[qh];
-      const bool some = l_tot[qh] != 0.0f;
       uint32_t w[C::DT][2];
 #pragma unroll
       for (int dt = 0; dt < C::DT; ++dt)

@@ -1,0 +1,40 @@
+"""Values of up to 2^127 in a paged cache, half of the largest finite one: the weighted sums that
+are not yet divided pass float32's range, the results do not."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from test_gpu_paged import BF16, F32, Case
+
+pytestmark = pytest.mark.gpu
+
+TOP = 2.0 ** 127
+
+
+def fill(c: Case, keys=None, rising=False):
+    """V is 0 but at the given keys of every sequence (all by default): there +-2^127 in turn over the
+    columns.  Scores are 0, so that every key weighs the same, or rise by 43 log2 units along the cache."""
+    c.q.zero_()
+    sign = torch.ones(c.q.shape[2])
+    sign[1::2] = -1.0
+    top = (TOP * sign).to(c.dtype)
+    for s, length in enumerate(c.b.kv_len):
+        for j in range(length):
+            p, slot = c.b.place(s, j)
+            c.v_pages[p, :, slot] = top if keys is None or j in keys else 0.0
+            if rising:
+                c.k_pages[p, :, slot, 0] = 30.0 * j / length
+    if rising:
+        c.q[:, :, 0] = 8.0 if c.q.shape[2] == 64 else 8.0 * 2 ** 0.5
+    return c
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("keys", [[0, 48, 80], [5, 3500, 7005]])
+def test_keys_of_several_waves_and_parts(dtype, d, keys):
+    """One key in a wave's block, in a part."""
+    for news in (1, 3):
+        c = Case([news], [9001], dtype=dtype, d=d, hk=1, group=7, page=64)
+        fill(c, keys).check_attention(heads=[0, 6])
