@@ -163,12 +163,15 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     paged_copy<C::N, NT>(dst + C::BLOCK + C::HALF, vp + c, voff);
   };
 
-  // The wave's blocks.  The rests of the probabilities meet a V element that is not finite as
-  // 0 or a negative number, which would make an infinity NaN: a wave whose O is not finite
-  // goes over its blocks again without them, and with weights of at most 1, so that values near
-  // the largest bf16 stay finite.
-  for (bool rests = true;; rests = false) {
-    const float raise = rests ? kRaise : 0.0f;
+  // The wave's blocks.  A wave whose O is not finite goes over them again, with a reference so
+  // far above the scores that its weights sum to at most 1: O then stays below the largest
+  // |V|, and is not finite where a V element is not.  The rests of the probabilities meet such
+  // an element as 0 or a negative number, which would make an infinity NaN: a third run leaves
+  // them out.
+  for (int run = 0;; ++run) {
+    const bool rests = run < 2;
+    const float raise = run == 0 ? kRaise : 0.0f;
+    const float lift = run == 0 ? 0.0f : float(32 - __builtin_clz(uint32_t(kBK * (t1 - t0) | 1)));
 #pragma unroll
     for (int x = 0; x < QT; ++x) {
       m_run[x] = -FLT_MAX;   // (finite: keys that score -inf get weight 0)
@@ -269,8 +272,8 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       for (int x = 0; x < QT; ++x) {
         mx[x] = fmaxf(fmaxf(s[0][x][0], s[0][x][1]), fmaxf(s[0][x][2], s[0][x][3]));
         mx[x] = fmaxf(mx[x], fmaxf(fmaxf(s[1][x][0], s[1][x][1]), fmaxf(s[1][x][2], s[1][x][3])));
-        mx[x] = max_across_groups(mx[x]) * t.scale_log2;
-        // the first block's max is the reference from then on, until a score passes it far
+        mx[x] = fmaf(max_across_groups(mx[x]), t.scale_log2, lift);
+        // the first block's max (lifted) is the reference from then on, until a score passes it far
         over |= mx[x] > (m_run[x] == -FLT_MAX ? m_run[x] : m_run[x] + raise);
       }
       if (__builtin_amdgcn_ballot_w64(over) != 0) {

@@ -38,3 +38,23 @@ def test_keys_of_several_waves_and_parts(dtype, d, keys):
     for news in (1, 3):
         c = Case([news], [9001], dtype=dtype, d=d, hk=1, group=7, page=64)
         fill(c, keys).check_attention(heads=[0, 6])
+
+
+# the keys of one wave's block, of several waves, of several parts, all
+KEYS = [range(4), range(0, 256, 16), range(5, 9000, 1000), None]
+
+
+@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("keys", KEYS)
+def test_few_rows(dtype, d, keys):
+    """A short cache (waves joined) and a long one (parts joined)."""
+    for news, length in (([1], 300), ([1], 9001), ([3], 9001)):
+        c = Case(news, [length], dtype=dtype, d=d, hk=1, group=7, page=64)
+        fill(c, keys).check_attention(heads=[0, 6])
+
+
+@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("news,length", [(1, 300), (20, 300), (1, 9001)])
+def test_few_rows_under_rising_scores(dtype, news, length):
+    fill(Case([news], [length], dtype=dtype, d=64, hk=1, group=2, page=64), rising=True).check_attention(rows=[0, news - 1])
