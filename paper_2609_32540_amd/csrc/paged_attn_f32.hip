@@ -6,8 +6,8 @@
 // the waves.  A block lies in one page (pages hold multiples of 16 tokens), K and V go
 // straight from global memory to the registers that the products read: the four summands
 // of a product are chosen to be consecutive in memory, so one 16-byte load per lane feeds
-// four products of each query tile.  The max is subtracted from a score before the factor
-// log2 e is applied: the largest key's exponent is then exactly 0.
+// four products of each query tile.  The reference is subtracted from a score before the factor
+// log2 e is applied, which rounds a difference of at most 4 above it instead of the score.
 //
 // One new token each of 16 sequences of up to 2300 tokens, 12 heads x 128: 52 us with the
 // join = 4.4 TB/s (bound by HBM; workgroups of eight waves, one per CU instead of two, 6 us more);
@@ -74,15 +74,6 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   }
   f32x4 o[QT][VH][4];
   float m_run[QT], l_run[QT];
-#pragma unroll
-  for (int x = 0; x < QT; ++x) {
-    m_run[x] = -FLT_MAX;   // (finite: a key whose score is -inf then gets weight 0)
-    l_run[x] = 0.0f;
-#pragma unroll
-    for (int h = 0; h < VH; ++h)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[x][h][e] = f32x4{};
-  }
 
   // lane i holds the page of block i of this wave's current 64 (a reload every 64 blocks)
   int page_of = -1;
@@ -126,145 +117,171 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
       for (int h = 0; h < VH; ++h) vreg[j][h] = load(p + 4 * (j * D + 64 * h), v_lane);
   };
 
-  int tb = t0 + wave, i = 0;
-  int page = -1;
-  int64_t off = 0;
-  if (tb < t1) {
-    load_pages(0);
-    page = __builtin_amdgcn_readlane(page_of, 0);
-    off = uniform(block_offset(page, blocks.key0(tb)));
-    load_k(off);
-    // (V behind K: the loop waits for K with V's loads in flight)
-    __builtin_amdgcn_sched_barrier(0);
-    load_v(off);
-  }
-  // Every turn issues the same loads in the same order, K of the next block, then its V (behind
-  // the last one of page 0): so the waits for K leave V's loads in flight and the other way round.
-  while (tb < t1) {
-    f32x4 s[QT];
+  // The wave's blocks.  A wave whose O is not finite goes over them again, with a reference so
+  // far above the scores that its weights sum to at most 1: O then stays below the largest
+  // |V|, and is not finite where a V element is not.
+  for (bool again = false;; again = true) {
+    const float raise = again ? 0.0f : kRaise;
+    const float lift = again ? (32 - __builtin_clz(uint32_t(kBK * (t1 - t0) | 1))) / kLog2e : 0.0f;
 #pragma unroll
-    for (int x = 0; x < QT; ++x) s[x] = f32x4{};
+    for (int x = 0; x < QT; ++x) {
+      m_run[x] = -FLT_MAX;   // (finite: a key whose score is -inf then gets weight 0)
+      l_run[x] = 0.0f;
 #pragma unroll
-    for (int k = 0; k < KT; ++k)
+      for (int h = 0; h < VH; ++h)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int x = 0; x < QT; ++x)
-          s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kreg[k][e], qreg[x][k][e], s[x], 0, 0, 0);
-    const int j0 = blocks.key0(tb), cur = page;
-    const int64_t cur_off = off;
-    // the next block: its K now, its V once this block's V is consumed
-    tb += kWaves;
-    ++i;
-    off = 0;
-    if (tb < t1) {
-      if ((i & 63) == 0) load_pages(i);
-      page = __builtin_amdgcn_readlane(page_of, i & 63);
-      off = uniform(block_offset(page, blocks.key0(tb)));
+        for (int e = 0; e < 4; ++e) o[x][h][e] = f32x4{};
     }
-    load_k(off);
-    __builtin_amdgcn_sched_barrier(0);
-
-    const bool edge = j0 + kBK > head_r.hi || cur < 0 || (j0 < tail_r.lo && j0 + kBK > b.anchor_tokens);
-    bool spread = false;
-    if (edge) {
+    int tb = t0 + wave, i = 0;
+    int page = -1;
+    int64_t off = 0;
+    if (tb < t1) {
+      load_pages(0);
+      page = __builtin_amdgcn_readlane(page_of, 0);
+      off = uniform(block_offset(page, blocks.key0(tb)));
+      load_k(off);
+      // (V behind K: the loop waits for K with V's loads in flight)
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(off);
+    }
+    // Every turn issues the same loads in the same order, K of the next block, then its V (behind
+    // the last one of page 0): so the waits for K leave V's loads in flight and the other way round.
+    while (tb < t1) {
+      f32x4 s[QT];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = j0 + 4 * grp + e;
+      for (int x = 0; x < QT; ++x) s[x] = f32x4{};
 #pragma unroll
-        for (int x = 0; x < QT; ++x) {
-          const bool seen = cur >= 0 && j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
-          s[x][e] = seen ? s[x][e] : -INFINITY;
-        }
-        const bool any = cur >= 0 && j < tail_r.hi && (j >= head_r.lo || j < b.anchor_tokens);
-        if (!any)
-#pragma unroll
-          for (int h = 0; h < VH; ++h) vreg[e][h] = f32x4{};
-      }
-      if (rows_differ) {
-        bool bad = false;
+      for (int k = 0; k < KT; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int h = 0; h < VH; ++h)
+          for (int x = 0; x < QT; ++x)
+            s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kreg[k][e], qreg[x][k][e], s[x], 0, 0, 0);
+      const int j0 = blocks.key0(tb), cur = page;
+      const int64_t cur_off = off;
+      // the next block: its K now, its V once this block's V is consumed
+      tb += kWaves;
+      ++i;
+      off = 0;
+      if (tb < t1) {
+        if ((i & 63) == 0) load_pages(i);
+        page = __builtin_amdgcn_readlane(page_of, i & 63);
+        off = uniform(block_offset(page, blocks.key0(tb)));
+      }
+      load_k(off);
+      __builtin_amdgcn_sched_barrier(0);
+
+      const bool edge = j0 + kBK > head_r.hi || cur < 0 || (j0 < tail_r.lo && j0 + kBK > b.anchor_tokens);
+      bool spread = false;
+      if (edge) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) bad |= !isfinite(vreg[e][h][w]);
-        spread = __builtin_amdgcn_ballot_w64(bad) != 0;
-        if (spread)
+        for (int e = 0; e < 4; ++e) {
+          const int j = j0 + 4 * grp + e;
+#pragma unroll
+          for (int x = 0; x < QT; ++x) {
+            const bool seen = cur >= 0 && j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
+            s[x][e] = seen ? s[x][e] : -INFINITY;
+          }
+          const bool any = cur >= 0 && j < tail_r.hi && (j >= head_r.lo || j < b.anchor_tokens);
+          if (!any)
+#pragma unroll
+            for (int h = 0; h < VH; ++h) vreg[e][h] = f32x4{};
+        }
+        if (rows_differ) {
+          bool bad = false;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int h = 0; h < VH; ++h)
 #pragma unroll
-              for (int w = 0; w < 4; ++w) vreg[e][h][w] = isfinite(vreg[e][h][w]) ? vreg[e][h][w] : 0.0f;
-      }
-    }
-
-    bool raised = false;
-    float mx[QT];
+              for (int w = 0; w < 4; ++w) bad |= !isfinite(vreg[e][h][w]);
+          spread = __builtin_amdgcn_ballot_w64(bad) != 0;
+          if (spread)
 #pragma unroll
-    for (int x = 0; x < QT; ++x) {
-      mx[x] = max_across_groups(fmaxf(fmaxf(s[x][0], s[x][1]), fmaxf(s[x][2], s[x][3])));
-      raised |= mx[x] > m_run[x] + kRaise;   // (-FLT_MAX + kRaise is -FLT_MAX)
-    }
-    if (__builtin_amdgcn_ballot_w64(raised) != 0) {
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int h = 0; h < VH; ++h)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) vreg[e][h][w] = isfinite(vreg[e][h][w]) ? vreg[e][h][w] : 0.0f;
+        }
+      }
+
+      bool raised = false;
+      float mx[QT];
 #pragma unroll
       for (int x = 0; x < QT; ++x) {
-        const float m_new = mx[x] > m_run[x] + kRaise ? mx[x] : m_run[x];
-        const float alpha = __builtin_amdgcn_exp2f((m_run[x] - m_new) * kLog2e);
-        m_run[x] = m_new;
-        l_run[x] *= alpha;
+        mx[x] = max_across_groups(fmaxf(fmaxf(s[x][0], s[x][1]), fmaxf(s[x][2], s[x][3]))) + lift;
+        raised |= mx[x] > m_run[x] + raise;   // (-FLT_MAX + raise is -FLT_MAX)
+      }
+      if (__builtin_amdgcn_ballot_w64(raised) != 0) {
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          const float m_new = mx[x] > m_run[x] + raise ? mx[x] : m_run[x];
+          const float alpha = __builtin_amdgcn_exp2f((m_run[x] - m_new) * kLog2e);
+          m_run[x] = m_new;
+          l_run[x] *= alpha;
+#pragma unroll
+          for (int h = 0; h < VH; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[x][h][e] *= alpha;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < QT; ++x) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s[x][e] = __builtin_amdgcn_exp2f((s[x][e] - m_run[x]) * kLog2e);
+        l_run[x] += (s[x][0] + s[x][1]) + (s[x][2] + s[x][3]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int h = 0; h < VH; ++h)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[x][h][e] *= alpha;
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int x = 0; x < QT; ++x)
+              o[x][h][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vreg[j][h][e], s[x][j], o[x][h][e], 0, 0, 0);
+      if (spread) {
+        // V elements that are not finite, for the rows that see their key
+#pragma unroll 1
+        for (int kk = 0; kk < kBK; ++kk) {
+          const int j = j0 + kk;
+          if (cur < 0 || j >= tail_r.hi) continue;
+          const float* vr = vpool + cur_off + kk * D;
+#pragma unroll
+          for (int x = 0; x < QT; ++x) {
+            float pr = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr = e == (kk & 3) ? s[x][e] : pr;
+            const float p = __shfl(pr, l16 + 16 * (kk >> 2));
+            const bool seen = j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
+#pragma unroll
+            for (int h = 0; h < VH; ++h)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                  const float v = vr[64 * h + 16 * grp + 4 * k + e];
+                  if (seen && !isfinite(v)) o[x][h][e][k] += p * v;
+                }
+          }
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(off);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    float any = 0.0f;
 #pragma unroll
-    for (int x = 0; x < QT; ++x) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        s[x][e] = __builtin_amdgcn_exp2f((s[x][e] - m_run[x]) * kLog2e);
-      l_run[x] += (s[x][0] + s[x][1]) + (s[x][2] + s[x][3]);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int x = 0; x < QT; ++x)
 #pragma unroll
       for (int h = 0; h < VH; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int x = 0; x < QT; ++x)
-            o[x][h][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vreg[j][h][e], s[x][j], o[x][h][e], 0, 0, 0);
-    if (spread) {
-      // V elements that are not finite, for the rows that see their key
-#pragma unroll 1
-      for (int kk = 0; kk < kBK; ++kk) {
-        const int j = j0 + kk;
-        if (cur < 0 || j >= tail_r.hi) continue;
-        const float* vr = vpool + cur_off + kk * D;
-#pragma unroll
-        for (int x = 0; x < QT; ++x) {
-          float pr = 0.0f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pr = e == (kk & 3) ? s[x][e] : pr;
-          const float p = __shfl(pr, l16 + 16 * (kk >> 2));
-          const bool seen = j < see[x].hi && (j >= see[x].lo || j < b.anchor_tokens);
-#pragma unroll
-          for (int h = 0; h < VH; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float v = vr[64 * h + 16 * grp + 4 * k + e];
-                if (seen && !isfinite(v)) o[x][h][e][k] += p * v;
-              }
-        }
-      }
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    load_v(off);
-    __builtin_amdgcn_sched_barrier(0);
+          for (int j = 0; j < 4; ++j) any = fmaf(o[x][h][e][j], 0.0f, any);
+    if (again || __builtin_amdgcn_ballot_w64(any != 0.0f) == 0) break;
   }
 
   // join the waves

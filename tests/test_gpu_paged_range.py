@@ -44,7 +44,7 @@ def test_keys_of_several_waves_and_parts(dtype, d, keys):
 KEYS = [range(4), range(0, 256, 16), range(5, 9000, 1000), None]
 
 
-@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("keys", KEYS)
 def test_few_rows(dtype, d, keys):
@@ -54,7 +54,7 @@ def test_few_rows(dtype, d, keys):
         fill(c, keys).check_attention(heads=[0, 6])
 
 
-@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("news,length", [(1, 300), (20, 300), (1, 9001)])
 def test_few_rows_under_rising_scores(dtype, news, length):
     fill(Case([news], [length], dtype=dtype, d=64, hk=1, group=2, page=64), rising=True).check_attention(rows=[0, news - 1])
