@@ -48,7 +48,8 @@ constexpr int kBlockQ = kPagedPromptRows;   // rows per workgroup
 static_assert(kBlockQ == kWaves * kWaveQ, "a tile is one workgroup");
 constexpr int kBK = 64;                     // keys per tile
 constexpr int kXcds = 8;
-constexpr float kSumLimit = 16.0f;          // checked pass: largest block sum of probabilities kept
+constexpr float kSumLimit = 16.0f;          // checked pass: largest sum of a lane's 8 probabilities of a
+                                            // block that is kept, in units of 2^-lift
 constexpr float kFastLimit = 0x1p64f;       // fast pass: largest row sum before the checked pass
 // passes of the key loop
 constexpr int kPassFast = 0;                // fixed reference, row sums of the rounded P on the matrix core
@@ -403,23 +404,26 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
 #pragma unroll
     for (int qh = 0; qh < kQH; ++qh) p_half(s, qh, pk, lb, std::true_type{});
   };
-  // The reference max is only raised when a block's probabilities (relative to
-  // it) sum past kSumLimit: then the reference is raised to the block's column
-  // max (O and l follow) and its probabilities are redone from the scores, which
-  // are still in registers.  Below the limit every probability is at most
-  // kSumLimit, so nothing overflows; infinities (scores far above the
-  // reference) also exceed it.  O is rescaled after the products of the previous
-  // block (issued in the same step) have been added into it.
+  // The reference is only raised when a lane's probabilities of a block (relative to
+  // it) sum past the limit: then it is raised to the block's column max plus lift
+  // (O and l follow) and the probabilities are redone from the scores, which
+  // are still in registers.  Infinities (scores far above the reference) also
+  // exceed the limit.  The lift makes all probabilities of a row sum to at most 1
+  // (64 2^-lift from each block's four lanes), so that O stays below the largest
+  // |V|.  O is rescaled after the products of the previous block (issued in the
+  // same step) have been added into it.
+  const int lift_bits = 6 + 32 - __builtin_clz(uint32_t(2 * n_tiles) | 1u);
+  const float lift = float(lift_bits), sum_limit = __builtin_amdgcn_ldexpf(kSumLimit, -lift_bits);
   auto check_blk = [&](const f32x4 (&s)[2][kQH], uint32_t (&pk)[kQH][4], float (&lb)[kQH])
       __attribute__((always_inline)) {
     bool over = false;
 #pragma unroll
-    for (int qh = 0; qh < kQH; ++qh) over |= lb[qh] > kSumLimit;
+    for (int qh = 0; qh < kQH; ++qh) over |= lb[qh] > sum_limit;
     if (__builtin_amdgcn_ballot_w64(over) != 0) {
       float alpha[kQH];
 #pragma unroll
       for (int qh = 0; qh < kQH; ++qh) {
-        const float m_new = fmaxf(m_run[qh], col_max(s, qh) * t.scale_log2);
+        const float m_new = fmaxf(m_run[qh], fmaf(col_max(s, qh), t.scale_log2, lift));
         alpha[qh] = __builtin_amdgcn_exp2f(m_run[qh] - m_new);
         l_run[qh] *= alpha[qh];
         m_run[qh] = m_new;
@@ -530,10 +534,12 @@ void paged_prompt_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
     k_read(slot(0), 1, ka);
     bool mask0 = edge(first_r, last_r, k0, bits0);   // tile n needs masks
     if (mask0) mask_blk(s_a, k0, bits0);
-    // reference max from the first block: its column max (O and l are zero); finite, so
-    // that keys that score -inf and rows that see none of the block get weight 0
+    // reference from the first block: its column max (O and l are zero), lifted in the
+    // checked pass; finite, so that keys that score -inf and rows that see none of the
+    // block get weight 0
 #pragma unroll
-    for (int qh = 0; qh < kQH; ++qh) m_run[qh] = fmaxf(col_max(s_a, qh) * t.scale_log2, -FLT_MAX);
+    for (int qh = 0; qh < kQH; ++qh)
+      m_run[qh] = fmaxf(fmaf(col_max(s_a, qh), t.scale_log2, kPass == kPassChecked ? lift : 0.0f), -FLT_MAX);
 #pragma unroll
     for (int qh = 0; qh < kQH; ++qh)
 #pragma unroll

@@ -58,3 +58,14 @@ def test_few_rows(dtype, d, keys):
 @pytest.mark.parametrize("news,length", [(1, 300), (20, 300), (1, 9001)])
 def test_few_rows_under_rising_scores(dtype, news, length):
     fill(Case([news], [length], dtype=dtype, d=64, hk=1, group=2, page=64), rising=True).check_attention(rows=[0, news - 1])
+
+
+@pytest.mark.parametrize("news,length,hk,form", [(700, 1000, 64, (0, 0, 256, 0)), (256, 24000, 4, (0, 0, 256, 1))])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("keys,rising", [(range(4), False), (range(5, 9000, 100), False), (None, False), (None, True)])
+def test_prompts(news, length, hk, form, d, keys, rising):
+    """The 256-row kernel, its keys in one part and in several; causal, with a window (no fast pass), and
+    as one block."""
+    c = fill(Case([news], [length], d=d, hk=hk, group=1, page=64), keys, rising)
+    for kw in (dict(), dict(window=length // 2), dict(block=True)):
+        c.check_attention(rows=[0, 100, news - 1], heads=[0, hk - 1], min_new=news, form=form, **kw)
