@@ -109,7 +109,7 @@ struct Launch {
   ff::PagedSplit split;
   int64_t tiles, items;  // at most this many per kv head
   size_t part_bytes;     // of its partial results
-  int waves;             // few rows, bf16: waves of a workgroup
+  int waves;             // few rows: waves of a workgroup
   bool once;             // and whether every sequence is one tile
 };
 struct Plan {
@@ -204,7 +204,7 @@ Plan make_plan(const ff_paged_desc& d) {
     set_items(d, &l, (keys + block - 1) / block, 1024 / block);
     // Short caches in more workgroups than two per CU: two waves each (no more of their
     // blocks than two waves' copies cover are left for four), twice as many sequences at once.
-    l.waves = keys <= 512 && l.tiles * d.num_kv_heads > 2 * cus ? 2 : 4;
+    l.waves = bf16 && keys <= 512 && l.tiles * d.num_kv_heads > 2 * cus ? 2 : 4;
     l.once = most <= l.rows;
   }
   if (many) {
@@ -228,8 +228,9 @@ Plan make_plan(const ff_paged_desc& d) {
 // The forms that the calling thread's last attention call took (exported as
 // ff_internal_last_paged, not part of the C ABI), so that a test can tell that it reached
 // the one it is about: rows of a tile of few rows (0: not launched) and whether its keys
-// could be cut, the same of many rows.
-thread_local int32_t last_paged[4] = {};
+// could be cut, the same of many rows; of few rows also the waves of a workgroup and
+// whether the keys are read past the caches.
+thread_local int32_t last_paged[6] = {};
 
 hipError_t run(const Launch& l, const ff_paged_desc& d, const ff::PagedBatch& b,
                const ff::PagedTensors& t, hipStream_t stream) {
@@ -249,7 +250,7 @@ hipError_t run(const Launch& l, const ff_paged_desc& d, const ff::PagedBatch& b,
 
 extern "C" {
 
-int32_t ff_internal_last_paged(int32_t field) { return field >= 0 && field < 4 ? last_paged[field] : -1; }
+int32_t ff_internal_last_paged(int32_t field) { return field >= 0 && field < 6 ? last_paged[field] : -1; }
 
 ff_status ff_paged_append(const ff_paged_desc* desc, const ff_paged_rope* rope, const void* q,
                           const void* k, const void* v, int64_t q_stride, int64_t k_stride,
@@ -355,8 +356,9 @@ ff_status ff_paged_attention(const ff_paged_desc* desc, const void* q, int64_t q
   t.scale = softmax_scale;
   t.scale_log2 = float(double(softmax_scale) * 1.4426950408889634);
   const hipStream_t hs = static_cast<hipStream_t>(stream);
-  const int32_t forms[4] = {p.few.rows, p.few.split.target > 0, p.many.rows, p.many.split.target > 0};
-  std::copy(forms, forms + 4, last_paged);
+  const int32_t forms[6] = {p.few.rows, p.few.split.target > 0, p.many.rows, p.many.split.target > 0,
+                            p.few.waves, p.few.once};
+  std::copy(forms, forms + 6, last_paged);
   hipError_t e = hipSuccess;
   if (p.few.rows > 0) e = run(p.few, d, b, t, hs);
   t.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.few.part_bytes);
