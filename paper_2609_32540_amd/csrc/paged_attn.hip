@@ -411,13 +411,14 @@ void paged_attn_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   }
 }
 
+// (tiles of 16 rows are chosen only where a sequence is one tile: once)
 template <int D, int QT, int W>
 hipError_t launch(bool once, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
                   int64_t items, hipStream_t stream) {
   const dim3 grid(unsigned(items * b.kv_heads));
-  if (once)
+  if (QT == 1 || once)
     hipLaunchKernelGGL((paged_attn_kernel<D, QT, W, true>), grid, dim3(64 * W), 0, stream, b, sp, t);
-  else
+  else if constexpr (QT > 1)
     hipLaunchKernelGGL((paged_attn_kernel<D, QT, W, false>), grid, dim3(64 * W), 0, stream, b, sp, t);
   return hipGetLastError();
 }

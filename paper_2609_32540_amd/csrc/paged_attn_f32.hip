@@ -337,13 +337,14 @@ void paged_attn_f32_kernel(PagedBatch b, PagedSplit sp, PagedTensors t) {
   }
 }
 
+// (tiles of 16 rows are chosen only where a sequence is one tile: once)
 template <int D, int QT>
 hipError_t launch(bool once, const PagedBatch& b, const PagedSplit& sp, const PagedTensors& t,
                   int64_t items, hipStream_t stream) {
   const dim3 grid(unsigned(items * b.kv_heads));
-  if (once)
+  if (QT == 1 || once)
     hipLaunchKernelGGL((paged_attn_f32_kernel<D, QT, true>), grid, dim3(kThreads), 0, stream, b, sp, t);
-  else
+  else if constexpr (QT > 1)
     hipLaunchKernelGGL((paged_attn_f32_kernel<D, QT, false>), grid, dim3(kThreads), 0, stream, b, sp, t);
   return hipGetLastError();
 }
