@@ -580,7 +580,7 @@ _PAGED_DTYPES = {torch.bfloat16: FF_DT_BF16, torch.float32: FF_DT_F32}
 _INT32_MAX = 2 ** 31 - 1
 
 
-def _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new) -> Exception:
+def _wrong_batch(n_tokens, k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new) -> Exception:
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages"), (q_start, "q_start"),
                     (kv_len, "kv_len"), (page_table, "page_table")):
         if not isinstance(t, torch.Tensor):
@@ -603,8 +603,8 @@ def _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new
         return ValueError("kv_len must be [n_seqs], q_start [n_seqs + 1], page_table [n_seqs][max_pages]")
     if dev.type != "cuda":
         return ValueError(f"the pool is on {dev}, expected a GPU")
-    if max(min_new, max_new) > _INT32_MAX:
-        return ValueError("min_new and max_new must fit in 32 bits")
+    if max(abs(min_new), abs(max_new), n_tokens, page_table.shape[1]) > _INT32_MAX:
+        return ValueError("min_new, max_new, the rows and the columns of page_table must fit in 32 bits")
     return ValueError("kv_len, q_start and the rows of page_table must be contiguous")
 
 
@@ -622,12 +622,13 @@ def _paged_desc(q_heads: int, n_tokens: int, k_pages: torch.Tensor, v_pages: tor
                 and kv_len.get_device() == dev and q_start.get_device() == dev
                 and page_table.get_device() == dev and n_starts == n_seqs + 1 and n_rows == n_seqs
                 and kv_len.is_contiguous() and q_start.is_contiguous() and (unit == 1 or max_pages <= 1)
-                and dev >= 0 and min_new <= _INT32_MAX and max_new <= _INT32_MAX)
+                and dev >= 0 and -_INT32_MAX <= min_new <= _INT32_MAX and -_INT32_MAX <= max_new <= _INT32_MAX
+                and n_tokens <= _INT32_MAX and max_pages <= _INT32_MAX)
         dtype = _PAGED_DTYPES[dt]
     except (ValueError, TypeError, AttributeError, KeyError):
         good = False
     if not good:
-        raise _wrong_batch(k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new)
+        raise _wrong_batch(n_tokens, k_pages, v_pages, q_start, kv_len, page_table, min_new, max_new)
     return PagedDesc(num_pages, page_tokens, q_heads, kv_heads, d, dtype, n_seqs, n_tokens, max_pages,
                      min_new, max_new, 0, stride if n_seqs > 1 else max_pages, q_start.data_ptr(),
                      kv_len.data_ptr(), page_table.data_ptr())
@@ -696,6 +697,11 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_page
     None without q.
     """
     pool = _pool(k_pages)
+    pairs = (0, 0, 0)
+    if rope_pairs is not None:
+        pairs = rope_pairs
+        if max(map(abs, pairs)) > _INT32_MAX:
+            raise ValueError("rope_pairs must fit in 32 bits")
     kp, ks, n, heads = _rows(k, pool, "k")
     vp, vs, v_rows, v_heads = _rows(v, pool, "v")
     if v_rows != n or v_heads != heads or heads != k_pages.shape[1]:
@@ -719,7 +725,6 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_page
             raise ValueError(f"positions must be a contiguous int32 [{n}][3] tensor on {k.device}")
         pp = positions.data_ptr()
     desc = _paged_desc(heads, n, k_pages, v_pages, q_start, kv_len, page_table, 0, 0)
-    pairs = rope_pairs if rope_pairs is not None else (0, 0, 0)
     rope = PagedRope(pairs[0], pairs[1], pairs[2], 0, rope_theta)
     dev = k.device
     _check(_call_on(dev.index, lib().ff_paged_append, ctypes.byref(desc), ctypes.byref(rope), qp, kp, vp, qs,
