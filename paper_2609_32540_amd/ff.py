@@ -665,6 +665,8 @@ def _rows(t: torch.Tensor, pool: Tuple[torch.dtype, int, int], name: str) -> Tup
 
 def _like(t: torch.Tensor, q: torch.Tensor, pool: Tuple[torch.dtype, int, int], name: str) -> int:
     """Pointer of a dense tensor of q's shape, in the pool's dtype and device."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
     if t.shape != q.shape or t.dtype is not pool[0] or t.get_device() != pool[1] or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {q.dtype} tensor of shape {tuple(q.shape)} on {q.device}")
     return t.data_ptr()
@@ -720,6 +722,8 @@ def paged_append(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_page
         raise ValueError("q_out without q")
     pp = None
     if positions is not None:
+        if not isinstance(positions, torch.Tensor):
+            raise TypeError("positions must be a torch.Tensor")
         if (positions.shape != (n, 3) or positions.dtype != torch.int32 or not positions.is_contiguous()
                 or positions.get_device() != k.get_device()):
             raise ValueError(f"positions must be a contiguous int32 [{n}][3] tensor on {k.device}")
@@ -763,6 +767,8 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     ref, L = ctypes.byref(desc), lib()
     wp, wn = None, 0
     if workspace is not None:
+        if not isinstance(workspace, torch.Tensor):
+            raise TypeError("workspace must be a torch.Tensor")
         if workspace.device != dev or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on the pool's device")
         wp, wn = workspace.data_ptr(), workspace.numel() * workspace.element_size()

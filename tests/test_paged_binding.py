@@ -1,4 +1,5 @@
-"""What the binding of the paged cache refuses before the library sees it: integers past 32 bits."""
+"""What the binding of the paged cache refuses before the library sees it: integers past 32 bits and
+arguments that are not tensors."""
 import pytest
 import torch
 
@@ -21,6 +22,13 @@ def test_rope_pairs_past_32_bits(pairs):
         ff.paged_append(k, k, pool, pool, *batch, rope_pairs=pairs)
 
 
+@pytest.mark.parametrize("kw", [dict(q_out=[1]), dict(positions=[[0, 0, 0]]), dict(positions=5)])
+def test_append_arguments_that_are_no_tensors(kw):
+    q, k, pool, batch = tensors("cpu")
+    with pytest.raises(TypeError, match="must be a torch.Tensor"):
+        ff.paged_append(k, k, pool, pool, *batch, q=q, **kw)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("hint", [dict(min_new=-2 ** 32), dict(max_new=1 - 2 ** 32), dict(min_new=1, max_new=2 ** 31)])
 def test_hints_past_32_bits(hint):
@@ -29,3 +37,11 @@ def test_hints_past_32_bits(hint):
         ff.paged_attention(q, pool, pool, *batch, **hint)
     with pytest.raises(ValueError, match="32 bits"):
         ff.paged_attention_workspace(q, pool, *batch, **hint)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kw", [dict(out=[1]), dict(lse=3.0), dict(workspace=b"1234")])
+def test_attention_arguments_that_are_no_tensors(kw):
+    q, _, pool, batch = tensors("cuda")
+    with pytest.raises(TypeError, match="must be a torch.Tensor"):
+        ff.paged_attention(q, pool, pool, *batch, **kw)
