@@ -60,7 +60,9 @@ extern "C" {
  *   max_pages        columns of page_table, >= 1; max_pages * page_tokens <= 2^30
  *   min_new, max_new bounds of a sequence's new tokens, 0 and 0: not known.  They choose
  *                    kernels: the results hold whatever they say.  max_new 1 for
- *                    decoding steps, min_new for batches of long prompts only
+ *                    decoding steps, min_new for batches of long prompts only.  max_pages
+ *                    chooses too, since lengths are on the device: a table no wider than
+ *                    the sequences need is the fastest for short ones
  *   table_stride     elements between rows of page_table (>= max_pages)
  *   q_start          device, n_seqs + 1 values
  *   kv_len           device, n_seqs values
@@ -126,10 +128,13 @@ size_t ff_paged_attention_workspace(const ff_paged_desc* desc);
  * [num_q_heads][head_dim].  lse (optional, device, [n_tokens][num_q_heads] float) receives
  * the base-2 log-sum-exp of each row's scaled scores, -inf for a row that sees none.
  * Arithmetic as ff_chunk_attention: bf16 products on the matrix cores with float32
- * accumulation, softmax in float32, probabilities (in sequences of few rows: and the rests of
- * that rounding) and output rounded to bf16 (nearest even); f32 float32 throughout.  How the
- * keys are split, and with it the last bits of a row, depends on the whole batch; the same
- * call gives the same bits.  One to four kernel launches, by the sizes in `desc`.
+ * accumulation, softmax in float32, output rounded to bf16 (nearest even); f32 float32
+ * throughout.  A bf16 probability enters the second product as two bf16 (2^-17) in the kernel
+ * of few rows, and as one (2^-8) in the kernel of many.  Which one a sequence meets, how its keys
+ * are split, and with both the last bits of a row, follow from the sizes of the whole batch,
+ * the table's columns and the hints among them; asking for the log-sum-exp may change them too.
+ * The same call gives the same bits.  Values of up to 2^127 give finite results, however many
+ * keys weigh alike.  One to four kernel launches, by the sizes in `desc`.
  * workspace (device, 16-byte aligned, ff_paged_attention_workspace() bytes) is the call's
  * until its work is done: calls that may overlap, graphs among them, need one each.  out
  * and lse must not overlap anything else. */

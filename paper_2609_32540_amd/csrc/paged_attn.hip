@@ -32,13 +32,17 @@
 // the error of its own rounding, 1.7e-3 (relative-L2) where probabilities of one bf16 give
 // 2.3e-3.  Scores, references, sums and O are float32.
 //
-// Measured (32/8 heads x 128, cold, joins included).  64 sequences of 150 to 12000 tokens:
-// 257 us = 5.9 TB/s, within 1% of the copies alone (the kernel without its operand reads and
-// products); read through the caches 284 us, so a key that no other tile reads is read past
-// them.  One sequence of 32773 tokens: 33 us, of which the join is 6 (1.3 its launch, 0.7 the
-// lookup); with twice the parts 42.  Two waves per workgroup, four workgroups per CU: 274
-// and 35, but 55 instead of 82 for 250 sequences of up to 308 tokens, 12 kv heads (and so
-// they are chosen there).
+// Range: an element of O is below the sum of weight times |V|, which a second run with weights
+// that sum to at most 1 keeps finite, and joins add outputs, not sums: |V| up to 2^127 gives
+// finite results.
+//
+// Measured (32/8 heads x 128, passes among others, joins included).  64 sequences of 150 to
+// 12000 tokens: 244 us = 6.2 TB/s, 242 the copies alone (the kernel without its operand reads and
+// products); read through the caches 274 us, so a key that no other tile reads is read past
+// them.  One sequence of 32774 tokens: 31 us, of which the join is 5 to 6 (1.3 its launch, 0.7
+// the lookup), 29 with the copies alone; 34 through the caches; 36 with twice the parts.  Two
+// waves per workgroup, four workgroups per CU: 258 and 31, but 45 instead of 63 for 250 sequences
+// of up to 308 tokens, 12 kv heads (and so they are chosen there).
 
 #include <hip/hip_runtime.h>
 

@@ -9,9 +9,9 @@
 // four products of each query tile.  The reference is subtracted from a score before the factor
 // log2 e is applied, which rounds a difference of at most 4 above it instead of the score.
 //
-// One new token each of 16 sequences of up to 2300 tokens, 12 heads x 128: 52 us with the
-// join = 4.4 TB/s (bound by HBM; workgroups of eight waves, one per CU instead of two, 6 us more);
-// one block of 2184 tokens over 8700 keys, 3 heads: 290 us = 101 TFLOP/s (the float32 matrix
+// One new token each of 16 sequences of up to 2300 tokens, 12 heads x 128: 51 us with the
+// join = 4.5 TB/s (bound by HBM; workgroups of eight waves, one per CU instead of two, 6 us more);
+// one block of 2184 tokens over 8736 keys, 3 heads: 284 us = 103 TFLOP/s (the float32 matrix
 // rate, 153 TFLOP/s in a large product; beside the products an item costs about 5 us, and nine
 // rounds of items are needed for an even load; the softmax among the next block's products, in
 // a pipelined turn, gains nothing, nor do tiles of the same keys on one XCD, whose L2 serves 95%).

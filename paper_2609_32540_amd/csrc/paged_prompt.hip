@@ -16,17 +16,23 @@
 //            tile ahead of their use; where rows see different keys, elements that are not
 //            finite too, which are added to the rows that see them at the end (their weight
 //            is positive: an infinity stays one).
-//   passes   the fast pass needs a first block that every row sees a key of, which a causal
-//            window does not give: those, and calls that want the log-sum-exp (the sum of the
-//            unrounded probabilities), run the checked pass at once.
-//   rounding probabilities as one bf16, the sums over the rounded values, as there: a second
-//            product for their rests would cost half of the products again.
+//   passes   the fast pass needs a first block (32 keys) that every row sees a key of, which a
+//            causal window does not give: those, and calls that want the log-sum-exp (the sum
+//            of the unrounded probabilities), run the checked pass at once.  Where holes cover
+//            the first block, or a block's window without anchors begins behind it in its tile,
+//            a workgroup runs both (two prompts with such holes 633 us).
+//   rounding probabilities as one bf16: a second product for their rests would cost half of the
+//            products again.  The fast pass divides by the sum of the rounded values, as there,
+//            the checked pass by that of the unrounded ones.
+//   range    O stays below the largest |V| in the checked pass, whose weights sum to at most 1;
+//            a fast pass that leaves float32's range is run again.
 //
-// Measured (32/8 heads x 128).  Prompts of 5003 and 3966 tokens, causal: 354 us = 1040 TFLOP/s
-// of the visible pairs; 16384 tokens as one block 1290 TFLOP/s.  40 heads, 4680 queries over
-// 28080 keys 2.33 ms (attn_bf16.hip over a ring 2.31).  A 64-key step takes 1.7 us, a tile about
-// 14 us beside its steps: workgroup launch, lookup and Q 7.5, the pages and the first copies
-// 6.5, which nothing covers, as all of a CU's LDS is one workgroup's.
+// Measured (32/8 heads x 128).  Prompts of 5003 and 3966 tokens, causal: 346 us = 1060 TFLOP/s
+// of the visible pairs, 370 in the checked pass; 16384 tokens as one block 1300 TFLOP/s.  40
+// heads, 4680 queries over 28080 keys 2.36 ms, 2.22 with pages of 64 tokens (attn_bf16.hip over
+// a ring 2.35).  A 64-key step takes 1.7 us, a tile about 14 us beside its steps: workgroup
+// launch, lookup and Q 7.5, the pages and the first copies 6.5, which nothing covers, as all of
+// a CU's LDS is one workgroup's.
 
 #include <hip/hip_runtime.h>
 
