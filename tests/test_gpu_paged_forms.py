@@ -61,6 +61,60 @@ def test_float32_few_tokens(d, new, group, form):
     assert forms() == form
 
 
+# ---- batches that the forms share --------------------------------------------------
+@gpu
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 64)])
+def test_long_caches_of_more_sequences_than_lanes(dtype, d):
+    """130 sequences, some of them cut into parts."""
+    rng = random.Random(d)
+    lens = [rng.choice([0, 1, 90, 1500, 3100]) for _ in range(130)]
+    c = Case([min(n, 1) for n in lens], lens, dtype=dtype, d=d, hk=1, group=2)
+    c.check_attention(max_new=1)
+    assert forms()[:2] == (16, 1)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_prompts_of_more_sequences_than_lanes(d):
+    rng = random.Random(d)
+    news = [rng.choice([0, 33, 64, 150]) for _ in range(100)]
+    lens = [n + rng.choice([0, 7, 200, 1000]) for n in news]
+    c = Case(news, lens, d=d, hk=16, group=4)
+    rows = sorted(rng.sample(range(c.rows), 40)) + [c.rows - 1]
+    for kw in (dict(), dict(window=100, anchors=20), dict(block=True)):
+        c.check_attention(rows=rows, heads=[0, 63], min_new=33, max_new=150, **kw)
+        assert forms()[:4] == (0, 0, 256, 0)
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_both_kernels_with_their_keys_in_parts(d):
+    """A slice of a prompt beside single tokens, long caches, few heads: both kernels leave partial
+    results in one workspace."""
+    c = Case([1000, 1, 1, 7], [16000, 9000, 300, 5000], d=d, hk=4, group=1, page=64)
+    for kw in (dict(), dict(block=True), dict(window=4000, anchors=500)):
+        c.check_attention(rows=[0, 255, 256, 999, 1000, 1001, 1002, 1008], heads=[0, 3], **kw)
+        assert forms()[:4] == (32, 1, 256, 1)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,news,lens,hk,kw", [
+    (BF16, [1], [9001], 2, dict(max_new=1)), (BF16, [1000, 1, 7], [16000, 9000, 5000], 4, {}),
+    (BF16, [1000], [16000], 4, dict(min_new=1000)), (F32, [1, 4], [5000, 3000], 2, {}), (F32, [200], [5000], 1, {})])
+def test_workspace_is_kept_to_and_not_read_before_it_is_written(dtype, news, lens, hk, kw):
+    c = Case(news, lens, dtype=dtype, d=64, hk=hk, group=1, page=64)
+    kp, vp, qs, kl, tb = c.on_gpu()
+    q = c.q.to(DEV)
+    n = ff.paged_attention_workspace(q, kp, qs, kl, tb, **kw)
+    assert n > 0
+    want = ff.paged_attention(q, kp, vp, qs, kl, tb, **kw)
+    for fill in (0xFF, 0x00):      # (0xFF: NaN)
+        wide = torch.full((4096 + n + 4096,), fill, dtype=torch.uint8, device=DEV)
+        got = ff.paged_attention(q, kp, vp, qs, kl, tb, workspace=wide[4096:4096 + n], **kw)
+        assert torch.equal(got, want)
+        assert (wide[:4096] == fill).all() and (wide[4096 + n:] == fill).all()
+
+
 # ---- appends -----------------------------------------------------------------------
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
