@@ -1,9 +1,11 @@
 """Values of up to 2^127 in a paged cache, half of the largest finite one: the weighted sums that
-are not yet divided pass float32's range, the results do not."""
+are not yet divided pass float32's range, the results do not.  Small ones keep their bits."""
 from __future__ import annotations
 
 import pytest
 import torch
+
+from paper_2609_32540_amd import ff
 
 from test_gpu_paged import BF16, F32, Case
 
@@ -69,3 +71,22 @@ def test_prompts(news, length, hk, form, d, keys, rising):
     c = fill(Case([news], [length], d=d, hk=hk, group=1, page=64), keys, rising)
     for kw in (dict(), dict(window=length // 2), dict(block=True)):
         c.check_attention(rows=[0, 100, news - 1], heads=[0, hk - 1], min_new=news, form=form, **kw)
+
+
+@pytest.mark.parametrize("dtype,news,length,hk,group", [
+    (BF16, 1, 9001, 1, 4), (F32, 1, 9001, 1, 4), (BF16, 5, 300, 2, 3), (F32, 40, 300, 2, 3), (BF16, 700, 1000, 64, 1),
+    (BF16, 256, 24000, 4, 1)])
+def test_small_values(dtype, news, length, hk, group):
+    """V of 2^-118: the result is that of V, scaled.  Products end at steps of 2^-149.  Where a reference is
+    lifted, by at most 16, a weight is above 2^-16 times what it is without, and these scores (standard
+    normal) keep the sum of n weights above n / 2^6: n half steps over that sum are 2^-128, 2^-10 of V's
+    unit.  The rest is a rounding of either side."""
+    c = Case([news], [length], dtype=dtype, d=64, hk=hk, group=group, page=64)
+    kp, vp, qs, kl, tb = c.on_gpu()
+    q = c.q.to("cuda")
+    u = 2.0 ** -8 if dtype == BF16 else 2.0 ** -22
+    for window in (-1, length):
+        for lse in (None, torch.empty(q.shape[:2], device="cuda")):
+            want = ff.paged_attention(q, kp, vp, qs, kl, tb, window=window, lse=lse, min_new=news).double()
+            got = ff.paged_attention(q, kp, vp * 2.0 ** -118, qs, kl, tb, window=window, lse=lse, min_new=news).double()
+            assert ((got * 2.0 ** 118 - want).abs() <= 2 * u * want.abs() + 2.0 ** -10).all()
